@@ -101,10 +101,10 @@ def draw(rng):
 
 
 def _spread(lo, hi, B, salt):
-    """B whole numbers from lo to hi, even over their logarithm, in an order of their own."""
-    if hi == 0:
-        return [0] * B
-    x = [int(round(math.exp(math.log(lo) + (math.log(hi) - math.log(lo)) * i / max(1, B - 1)))) for i in range(B)]
+    """B whole numbers from lo to hi, even over their logarithm, in an order of their own (one: hi)."""
+    if hi == 0 or B == 1:
+        return [hi] * B
+    x = [int(round(math.exp(math.log(lo) + (math.log(hi) - math.log(lo)) * i / (B - 1)))) for i in range(B)]
     random.Random(salt).shuffle(x)
     return x
 
