@@ -10,7 +10,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 OUT = os.path.join(_HERE, "libspt.so")
 SOURCES = ("api.cpp", "profile.cpp", "router.hip", "bucket.hip", "ffn.hip", "ffn_scatter.hip", "ffn_wide.hip",
-           "lora.hip", "mha.hip", "mha_dense.hip", "calibrate.hip")
+           "lora.hip", "mha.hip", "mha_dense.hip", "attn_prompt.hip", "attn_prompt_bwd.hip", "attn_cache.hip", "calibrate.hip")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 # (accumulators that vector instructions add to the LDS slab: in vector registers, not copied out of the accumulator file; 8192 tokens,

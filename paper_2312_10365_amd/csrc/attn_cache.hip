@@ -1,0 +1,624 @@
+// The paged cache of keys and values, and the attention of single tokens over it (include/spt_attn.h).
+#include "attn_common.hpp"
+
+using namespace spt;
+
+namespace {
+
+struct CacheArgs {
+  char *Kc, *Vc;
+  uint8_t *ks, *vs;
+  const int32_t* table;
+  int pages, page_shift, Hk, B, max_pages;
+};
+
+// ------------------------------------------------------------------------------------------
+// Writing and reading rows.  A wavefront takes one row of the packed tensors, all key heads of K and V; DH / 8 lanes a
+// head, 16 bytes of the packed row each.  Bytes in and out once; nothing to compute but a row's largest magnitude.
+
+struct RowArgs {
+  CacheArgs c;
+  AttnRows K, V;
+  const int32_t *start, *cu;
+  int T;
+};
+
+// Sequence of packed row r: the number of sequences that end at or before it.  64 at a time.
+__device__ __forceinline__ int sequence_of(const int32_t* cu, int B, int r) {
+  const int lane = threadIdx.x & 63;
+  int b = 0;
+  for (int b0 = 0; b0 < B; b0 += 64) {
+    const bool ends = b0 + lane < B && cu[b0 + lane + 1] <= r;
+    b += __builtin_popcountll(__ballot(ends));
+  }
+  return b;
+}
+
+// Where token `pos` of sequence b lies, as (page Hk page-size + place in it) of head 0; negative: nowhere.
+__device__ __forceinline__ int64_t token_place(const CacheArgs& c, int b, int64_t pos) {
+  if (pos < 0 || pos >= ((int64_t)c.max_pages << c.page_shift)) return -1;
+  const int p = c.table[(int64_t)b * c.max_pages + (int)(pos >> c.page_shift)];
+  if (p < 0 || p >= c.pages) return -1;
+  return (((int64_t)p * c.Hk) << c.page_shift) + (pos & ((1 << c.page_shift) - 1));
+}
+
+// largest of LANES neighbouring lanes' values
+template <int LANES>
+__device__ __forceinline__ uint32_t lanes_max(uint32_t x) {
+#pragma unroll
+  for (int o = 1; o < LANES; o <<= 1) x = max(x, (uint32_t)__shfl_xor((int)x, o));
+  return x;
+}
+
+// Exponent byte of a row whose largest finite magnitude is the bf16 (or fp32) with these bits: the least e >= -127 with
+// that magnitude <= 448 2^e, plus 127.  448 = 1.75 2^8: the fraction decides between two exponents.
+__device__ __forceinline__ int row_exponent(uint32_t bits) {
+  if (bits < 0x00800000u) return 0;                        // below 2^-126: e = -127
+  return max(0, (int)(bits >> 23) - 8 + ((bits & 0x7FFFFFu) > 0x600000u ? 1 : 0));
+}
+
+// 4 values -> 4 codes.  x 2^-e is exact and at most 448, so only the conversion rounds (nearest even).
+__device__ __forceinline__ uint32_t code4(const float* x) {
+  int w = __builtin_amdgcn_cvt_pk_fp8_f32(x[0], x[1], 0, false);
+  w = __builtin_amdgcn_cvt_pk_fp8_f32(x[2], x[3], w, true);
+  return (uint32_t)w;
+}
+
+template <int DH, bool E4M3>
+__global__ __launch_bounds__(256) void cache_write_kernel(const RowArgs a) {
+  constexpr int LANES = DH / 8, HEADS = 64 / LANES;
+  const int lane = threadIdx.x & 63, r = blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (r >= a.T) return;
+  const int b = sequence_of(a.cu, a.c.B, r);
+  if (b >= a.c.B || r < a.cu[b]) return;
+  const int64_t place = token_place(a.c, b, (int64_t)a.start[b] + r - max(a.cu[b], 0));
+  if (place < 0) return;
+  const int piece = lane % LANES;
+  for (int n = lane / LANES; n < 2 * a.c.Hk; n += HEADS) {
+    const bool v = n >= a.c.Hk;
+    const int hk = v ? n - a.c.Hk : n;
+    const AttnRows& src = v ? a.V : a.K;
+    const u32x4 x = *reinterpret_cast<const u32x4*>(src.p + r * src.row + hk * src.head + piece * 16);
+    const int64_t at = place + ((int64_t)hk << a.c.page_shift);
+    char* dst = v ? a.c.Vc : a.c.Kc;
+    if (!E4M3) {
+      *reinterpret_cast<u32x4*>(dst + at * (DH * 2) + piece * 16) = x;
+      continue;
+    }
+    uint32_t top = 0;
+    float f[8];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      f[2 * e] = lo_bf16(x[e]);
+      f[2 * e + 1] = hi_bf16(x[e]);
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const uint32_t mag = __float_as_uint(f[e]) & 0x7FFFFFFFu;
+      if (mag < 0x7F800000u) top = max(top, mag);
+    }
+    const int byte = row_exponent(lanes_max<LANES>(top));
+    const float most = byte == 247 ? 240.f : 448.f;         // (256 2^120 is no bf16)
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      f[e] = (__float_as_uint(f[e]) & 0x7F800000u) == 0x7F800000u ? __builtin_nanf("")
+                                                                  : __builtin_amdgcn_fmed3f(__builtin_ldexpf(f[e], 127 - byte), -most, most);
+    *reinterpret_cast<uint2*>(dst + at * DH + piece * 8) = make_uint2(code4(f), code4(f + 4));
+    if (piece == 0) (v ? a.c.vs : a.c.ks)[at] = (uint8_t)byte;
+  }
+}
+
+typedef __bf16 pair_bf16 __attribute__((ext_vector_type(2)));
+// 4 codes -> 4 bf16 of the values code * scale
+__device__ __forceinline__ uint2 uncode4(uint32_t w, float scale) {
+  const pair_bf16 lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, false), hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, true);
+  return make_uint2(__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi));
+}
+// 4 codes and the exponent byte of their row -> 4 bf16 (exact)
+__device__ __forceinline__ uint2 held4(uint32_t w, int byte) {
+  const uint2 x = uncode4(w, 1.f);
+  auto at = [&](float v) { return __builtin_ldexpf(v, byte - 127); };
+  return make_uint2(pack_bf16x2(at(lo_bf16(x.x)), at(hi_bf16(x.x))), pack_bf16x2(at(lo_bf16(x.y)), at(hi_bf16(x.y))));
+}
+
+template <int DH, bool E4M3>
+__global__ __launch_bounds__(256) void cache_read_kernel(const RowArgs a) {
+  constexpr int LANES = DH / 8, HEADS = 64 / LANES;
+  const int lane = threadIdx.x & 63, r = blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (r >= a.T) return;
+  const int b = sequence_of(a.cu, a.c.B, r);
+  if (b >= a.c.B || r < a.cu[b]) return;
+  const int64_t place = token_place(a.c, b, (int64_t)a.start[b] + r - max(a.cu[b], 0));
+  const int piece = lane % LANES;
+  for (int n = lane / LANES; n < 2 * a.c.Hk; n += HEADS) {
+    const bool v = n >= a.c.Hk;
+    const int hk = v ? n - a.c.Hk : n;
+    const AttnRows& to = v ? a.V : a.K;
+    const char* src = v ? a.c.Vc : a.c.Kc;
+    const int64_t at = place + ((int64_t)hk << a.c.page_shift);
+    u32x4 x = {0, 0, 0, 0};
+    if (place >= 0) {
+      if (!E4M3) {
+        x = *reinterpret_cast<const u32x4*>(src + at * (DH * 2) + piece * 16);
+      } else {
+        const uint2 w = *reinterpret_cast<const uint2*>(src + at * DH + piece * 8);
+        const int byte = (v ? a.c.vs : a.c.ks)[at];
+        const uint2 lo = held4(w.x, byte), hi = held4(w.y, byte);
+        x = u32x4{lo.x, lo.y, hi.x, hi.y};
+      }
+    }
+    *reinterpret_cast<u32x4*>(to.p + r * to.row + hk * to.head + piece * 16) = x;
+  }
+}
+
+// ------------------------------------------------------------------------------------------
+// Decoding.  The cache is read once; everything else is small.  An item is a key head of a sequence with up to 16 of the
+// query heads that read it (the columns of a 16 x 16 x 32 product), a unit 32 tokens of an item.  The units of all items stand in one line, and
+// every workgroup takes an equal stretch of it, whatever the lengths: an item that lies within one workgroup's stretch is
+// finished there, the others leave a partial result (maximum, sum, unnormalised output) per workgroup, which a second launch
+// joins in the order of the cache.  At most the first and the last item of a stretch are partial: two slots a workgroup.
+// In a workgroup the four wavefronts take turns at the units of an item, each with a ring of two units in LDS of its own,
+// filled by asynchronous copies: no barrier but at an item's end.  Scores are formed transposed (rows: tokens), so that
+// a lane holds the weights of one query as the second product wants them; a weight goes into it as the sum of two bf16 (the
+// matrix cores have nothing else to do), so the weights are exact to 2^-17.  8-bit codes become bf16 in registers, exactly; the rows' exponents are
+// applied to the scores and to the weights.
+
+constexpr int kUnit = 32, kDecodeWaves = 4;
+
+struct DecodeArgs {
+  CacheArgs c;
+  AttnRows Q, Y;
+  const int32_t* lens;
+  float *part, *stat;             // [slots][rows][DH], [slots][rows][2] (maximum, sum)
+  int H, G, sets, rows;           // sets of at most 16 heads of a group; rows of a slot
+  int workgroups;
+  float cs;                       // scale log2 e
+};
+
+__device__ __forceinline__ int seq_units(const DecodeArgs& a, int b) {
+  const int cap = a.c.max_pages << a.c.page_shift;
+  return (min(max(a.lens[b], 0), cap) + kUnit - 1) / kUnit;
+}
+
+struct Line { int total, share; };
+// Units of all sequences, and a workgroup's part of them.
+__device__ __forceinline__ Line unit_line(const DecodeArgs& a) {
+  int n = 0;
+  for (int b = threadIdx.x & 63; b < a.c.B; b += 64) n += seq_units(a, b);
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) n += __shfl_xor(n, o);
+  n = __builtin_amdgcn_readfirstlane(n) * a.c.Hk * a.sets;
+  return {n, max(1, (n + a.workgroups - 1) / a.workgroups)};
+}
+// First unit of sequence b's items
+__device__ __forceinline__ int units_before(const DecodeArgs& a, int b) {
+  int n = 0;
+  for (int x = threadIdx.x & 63; x < b; x += 64) n += seq_units(a, x);
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) n += __shfl_xor(n, o);
+  return __builtin_amdgcn_readfirstlane(n) * a.c.Hk * a.sets;
+}
+
+template <int DH, bool E4M3>
+struct DecodeTile {
+  static constexpr int RB = E4M3 ? DH : DH * 2;            // bytes of a row
+  static constexpr int BYTES = kUnit * RB;                 // of a unit's K or V
+  static constexpr int COPIES = BYTES / 1024;
+  static constexpr int STAGE = 2 * BYTES + (E4M3 ? 256 : 0);
+  static constexpr int LOADS = 2 * COPIES + (E4M3 ? 1 : 0);
+  static constexpr int RING = 2 * STAGE;
+};
+
+template <int DH, bool E4M3>
+__global__ __launch_bounds__(64 * kDecodeWaves) void decode_kernel(const DecodeArgs a) {
+  typedef DecodeTile<DH, E4M3> T;
+  constexpr int RB = T::RB, KS = DH / 32, DT = DH / 16;
+  extern __shared__ __align__(256) char smem[];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int q = lane & 15, c = lane >> 4;
+  char* ring = smem + wave * T::RING;
+
+  const Line line = unit_line(a);
+  int u = blockIdx.x * line.share;
+  const int uend = min(line.total, u + line.share);
+  if (u >= uend) return;
+  // the sequence of unit u
+  int b = 0, rem = u;
+  {
+    const int per = a.c.Hk * a.sets;
+    int before = 0;
+    for (int b0 = 0; b0 < a.c.B; b0 += 64) {
+      int incl = b0 + lane < a.c.B ? seq_units(a, b0 + lane) * per : 0;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const int up = __shfl_up(incl, o);
+        if (lane >= o) incl += up;
+      }
+      const int total = __builtin_amdgcn_readlane(incl, 63);
+      if (u - before < total) {
+        const int src = __builtin_ctzll(__ballot(incl > u - before));
+        b = b0 + src;
+        rem = u - before - (src > 0 ? __builtin_amdgcn_readlane(incl, src - 1) : 0);
+        break;
+      }
+      before += total;
+    }
+  }
+
+  for (bool first_item = true; u < uend; first_item = false) {
+    const int cap = a.c.max_pages << a.c.page_shift;
+    const int len = min(max(uniform_load(a.lens + b), 0), cap), units = (len + kUnit - 1) / kUnit;
+    if (units == 0) { ++b; continue; }
+    const int item = rem / units, t0 = rem - item * units, t1 = min(units, t0 + uend - u);
+    const int hk = item / a.sets, head0 = hk * a.G + (item - hk * a.sets) * 16, heads = min(16, (hk + 1) * a.G - head0);
+
+    bf16x8 qf[KS];
+    const char* qrow = a.Q.p + b * a.Q.row + (int64_t)(head0 + min(q, heads - 1)) * a.Q.head;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) qf[s] = *reinterpret_cast<const bf16x8*>(qrow + s * 64 + c * 16);
+
+    const int32_t* table = a.c.table + (int64_t)b * a.c.max_pages;
+    // copies of unit t into a stage; returns which of its 32 tokens are there
+    auto fetch = [&](int t, int stage) -> uint32_t {
+      const uint32_t at = lds_addr(ring + stage * T::STAGE);
+      uint32_t there = 0;
+      int64_t row[2];
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        const int pos = t * kUnit + 16 * half;
+        int page = pos < len ? uniform_load(table + (pos >> a.c.page_shift)) : -1;
+        if (page >= 0 && page < a.c.pages) there |= (len - pos >= 16 ? 0xFFFFu : (1u << (len - pos)) - 1u) << (16 * half);
+        else page = 0;
+        row[half] = ((((int64_t)page * a.c.Hk) + hk) << a.c.page_shift) + (pos & ((1 << a.c.page_shift) - 1));
+      }
+#pragma unroll
+      for (int n = 0; n < T::COPIES; ++n) {
+        const int r = n * (1024 / RB) + lane / (RB / 16);    // row of the unit; 16 n' .. of one half
+        const int half = n * (1024 / RB) / 16;
+        const uint32_t off = (uint32_t)(r - 16 * half) * RB + (((uint32_t)lane % (RB / 16)) ^ chunk_swizzle<RB>(r)) * 16;
+        dma16_at(a.c.Kc + row[half] * RB, off, at + n * 1024);
+        dma16_at(a.c.Vc + row[half] * RB, off, at + T::BYTES + n * 1024);
+      }
+      if (E4M3) {                                            // lanes 0-7: exponents of the keys, 8-15: of the values
+        const int half = (lane >> 2) & 1;
+        dma4(((lane & 8) ? a.c.vs : a.c.ks) + row[half] + 4 * (lane & 3), at + 2 * T::BYTES);
+      }
+      return there;
+    };
+
+    f32x4 o[DT];
+#pragma unroll
+    for (int d = 0; d < DT; ++d) o[d] = f32x4{0.f, 0.f, 0.f, 0.f};
+    float m = -INFINITY, neg_m = 0.f, l = 0.f;
+
+    wait_vmcnt<0>();                                         // (stores of the item before)
+    int t = t0 + wave;
+    uint32_t there = 0, next = 0;
+    if (t < t1) there = fetch(t, 0);
+    for (int stage = 0; t < t1; t += kDecodeWaves, stage ^= 1, there = next) {
+      if (t + kDecodeWaves < t1) {
+        next = fetch(t + kDecodeWaves, stage ^ 1);
+        wait_vmcnt<T::LOADS>();
+      } else {
+        wait_vmcnt<0>();
+      }
+      wave_lds_fence();
+      char* kt = ring + stage * T::STAGE;
+      char* vt = kt + T::BYTES;
+      if (there != 0xFFFFFFFFu) {                            // 0 times what lies behind the last token may be NaN
+        for (int n = 0; n < T::COPIES; ++n) {
+          const int r = n * (1024 / RB) + lane / (RB / 16);
+          if (!((there >> r) & 1)) *reinterpret_cast<u32x4*>(vt + n * 1024 + lane * 16) = u32x4{0, 0, 0, 0};
+        }
+        wave_lds_fence();
+      }
+      f32x4 s[2];
+#pragma unroll
+      for (int kt2 = 0; kt2 < 2; ++kt2) {
+        s[kt2] = f32x4{0.f, 0.f, 0.f, 0.f};
+        const int r = 16 * kt2 + q;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          bf16x8 f;
+          if (E4M3) {
+            const uint32_t piece = 4 * ks + c;
+            const uint2 w = *reinterpret_cast<const uint2*>(kt + r * RB + ((piece >> 1) ^ chunk_swizzle<RB>(r)) * 16 + (piece & 1) * 8);
+            const uint2 lo = uncode4(w.x, 1.f), hi = uncode4(w.y, 1.f);
+            f = as_bf16x8(u32x4{lo.x, lo.y, hi.x, hi.y});
+          } else {
+            f = *reinterpret_cast<const bf16x8*>(kt + r * RB + ((uint32_t)(4 * ks + c) ^ chunk_swizzle<RB>(r)) * 16);
+          }
+          s[kt2] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, qf[ks], s[kt2], 0, 0, 0);
+        }
+      }
+      uint32_t kb[2] = {0, 0}, vb[2] = {0, 0};               // exponents of the lane's tokens 16 kt2 + 4 c + e
+      if (E4M3) {
+        const uint32_t* ex = reinterpret_cast<const uint32_t*>(kt + 2 * T::BYTES);
+        kb[0] = ex[c]; kb[1] = ex[4 + c];
+        vb[0] = ex[8 + c]; vb[1] = ex[12 + c];
+      }
+      float x[8], top = -INFINITY;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        float v = s[e >> 2][e & 3] * a.cs;
+        if (E4M3) v = __builtin_ldexpf(v, (int)((kb[e >> 2] >> (8 * (e & 3))) & 255u) - 127);
+        x[e] = (there >> (16 * (e >> 2) + 4 * c + (e & 3))) & 1 ? v : -INFINITY;
+        top = fmaxf(top, x[e]);
+      }
+      top = fmaxf(top, __shfl_xor(top, 16));
+      top = fmaxf(top, __shfl_xor(top, 32));
+      if (__any(top > m)) {
+        const float mn = fmaxf(m, top), ms = mn == -INFINITY ? 0.f : mn, alpha = __builtin_amdgcn_exp2f(m - ms);
+        m = mn;
+        neg_m = -ms;
+        l *= alpha;
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[d][e] *= alpha;
+      }
+      float w[8], rest[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float p = __builtin_amdgcn_exp2f(x[e] + neg_m);
+        l += p;
+        w[e] = p;
+        if (E4M3) {
+          w[e] = __builtin_ldexpf(p, (int)((vb[e >> 2] >> (8 * (e & 3))) & 255u) - 127);
+          if (!((there >> (16 * (e >> 2) + 4 * c + (e & 3))) & 1)) w[e] = 0.f;
+        }
+      }
+      const bf16x8 hi = pack8(w);
+      const u32x4 hw = __builtin_bit_cast(u32x4, hi);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) rest[e] = w[e] - (e & 1 ? hi_bf16(hw[e >> 1]) : lo_bf16(hw[e >> 1]));
+      const bf16x8 lo = pack8(rest);
+      const int sl = lane & 15;
+#pragma unroll
+      for (int d = 0; d < DT; ++d) {
+        bf16x8 f;
+        if (E4M3) {
+          const int rr = sl >> 1, r = 4 * c + (rr & 3) + 16 * (rr >> 2);
+          typedef int v2i __attribute__((ext_vector_type(2)));
+          const v2i w8 = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
+              (__attribute__((address_space(3))) v2i*)(uintptr_t)(vt + r * RB + ((uint32_t)d ^ chunk_swizzle<RB>(r)) * 16 + (sl & 1) * 8));
+          const uint2 f0 = uncode4((uint32_t)w8[0], 1.f), f1 = uncode4((uint32_t)w8[1], 1.f);
+          f = as_bf16x8(u32x4{f0.x, f0.y, f1.x, f1.y});
+        } else {
+          const int r = 4 * c + (sl >> 2);
+          const uint32_t chunk = 2 * d + ((sl & 3) >> 1);
+          f = tr_read_frag(vt + r * RB + (chunk ^ chunk_swizzle<RB>(r)) * 16 + (sl & 1) * 8,
+                           vt + (r + 16) * RB + (chunk ^ chunk_swizzle<RB>(r + 16)) * 16 + (sl & 1) * 8);
+        }
+        o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, hi, o[d], 0, 0, 0);
+        o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, lo, o[d], 0, 0, 0);
+      }
+      wave_lds_fence();
+    }
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+
+    // the four wavefronts' results, joined in order
+    __syncthreads();
+    float* ml = reinterpret_cast<float*>(smem);              // [wave][16][2]
+    float* os = ml + kDecodeWaves * 32;                      // [wave][16][DH + 4]
+    constexpr int LD = DH + 4;
+    if (c == 0) { ml[(wave * 16 + q) * 2] = m; ml[(wave * 16 + q) * 2 + 1] = l; }
+#pragma unroll
+    for (int d = 0; d < DT; ++d) *reinterpret_cast<f32x4*>(os + (wave * 16 + q) * LD + 16 * d + 4 * c) = o[d];
+    __syncthreads();
+    const bool whole = t0 == 0 && t1 == units;
+    const int slot = 2 * blockIdx.x + (first_item ? 0 : 1);
+    for (int n = threadIdx.x; n < heads * (DH / 4); n += 64 * kDecodeWaves) {
+      const int row = n / (DH / 4), d4 = n % (DH / 4);
+      float M = -INFINITY;
+#pragma unroll
+      for (int w2 = 0; w2 < kDecodeWaves; ++w2) M = fmaxf(M, ml[(w2 * 16 + row) * 2]);
+      const float ms = M == -INFINITY ? 0.f : M;
+      f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+      float L = 0.f;
+#pragma unroll
+      for (int w2 = 0; w2 < kDecodeWaves; ++w2) {
+        const float f = __builtin_amdgcn_exp2f(ml[(w2 * 16 + row) * 2] - ms);
+        L = fmaf(f, ml[(w2 * 16 + row) * 2 + 1], L);
+        const f32x4 x = *reinterpret_cast<const f32x4*>(os + (w2 * 16 + row) * LD + 4 * d4);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[e] = fmaf(f, x[e], sum[e]);
+      }
+      if (whole) {
+        const float inv = L == 0.f ? 0.f : 1.f / L;
+        *reinterpret_cast<uint2*>(a.Y.p + b * a.Y.row + (int64_t)(head0 + row) * a.Y.head + d4 * 8) =
+            make_uint2(pack_bf16x2(sum[0] * inv, sum[1] * inv), pack_bf16x2(sum[2] * inv, sum[3] * inv));
+      } else {
+        const int64_t at = (int64_t)slot * a.rows + row;
+        *reinterpret_cast<f32x4*>(a.part + at * DH + 4 * d4) = sum;
+        if (d4 == 0) { a.stat[at * 2] = M; a.stat[at * 2 + 1] = L; }
+      }
+    }
+    __syncthreads();
+    u += t1 - t0;
+    rem += t1 - t0;
+    if (rem == units * a.c.Hk * a.sets) { ++b; rem = 0; }
+  }
+}
+
+// One wavefront per query head: the partial results of its item in the order of the cache, or zeros without a key.
+template <int DH>
+__global__ __launch_bounds__(256) void decode_join_kernel(const DecodeArgs a) {
+  const int lane = threadIdx.x & 63, row = blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (row >= a.c.B * a.H) return;
+  const int b = row / a.H, head = row - b * a.H, hk = head / a.G, g = head - hk * a.G;
+  const int units = seq_units(a, b);
+  char* y = a.Y.p + b * a.Y.row + (int64_t)head * a.Y.head;
+  constexpr int N = DH / 64;
+  if (units == 0) {
+#pragma unroll
+    for (int d = 0; d < N; ++d) reinterpret_cast<uint16_t*>(y)[N * lane + d] = 0;
+    return;
+  }
+  const Line line = unit_line(a);
+  const int u0 = units_before(a, b) + (hk * a.sets + g / 16) * units, u1 = u0 + units;
+  const int w0 = u0 / line.share, w1 = (u1 - 1) / line.share;
+  if (w0 == w1) return;                                      // finished where it was read
+  float M = -INFINITY, L = 0.f, sum[N] = {};
+  for (int w = w0; w <= w1; ++w) {
+    const int slot = 2 * w + (w == w0 && w0 * line.share != u0 ? 1 : 0);
+    const int64_t at = (int64_t)slot * a.rows + g % 16;
+    const float m = a.stat[at * 2], l = a.stat[at * 2 + 1], mn = fmaxf(M, m), ms = mn == -INFINITY ? 0.f : mn;
+    const float f = __builtin_amdgcn_exp2f(m - ms), old = __builtin_amdgcn_exp2f(M - ms);
+    M = mn;
+    L = fmaf(L, old, f * l);
+#pragma unroll
+    for (int d = 0; d < N; ++d) sum[d] = fmaf(sum[d], old, f * a.part[at * DH + N * lane + d]);
+  }
+  const float inv = L == 0.f ? 0.f : 1.f / L;
+#pragma unroll
+  for (int d = 0; d < N; ++d) reinterpret_cast<uint16_t*>(y)[N * lane + d] = (uint16_t)pack_bf16x2(sum[d] * inv, 0.f);
+}
+
+// ------------------------------------------------------------------------------------------
+int check_cache(const spt_cache_shape_t* s) {
+  if (!s) return SPT_ERR_ARG;
+  if (s->pages < 1 || s->page < 1 || s->Hk < 1 || s->dh < 1 || s->B < 1 || s->max_pages < 1) return SPT_ERR_ARG;
+  if ((int64_t)s->max_pages * s->page > INT_MAX) return SPT_ERR_ARG;
+  if (s->page < 16 || s->page > 256 || (s->page & (s->page - 1)) || (s->dh != 64 && s->dh != 128)) return SPT_ERR_UNSUPPORTED;
+  if ((s->format != SPT_CACHE_BF16 && s->format != SPT_CACHE_E4M3) || s->B > 65535 || s->Hk > 65535) return SPT_ERR_UNSUPPORTED;
+  return SPT_OK;
+}
+
+int check_pool(const spt_cache_shape_t& s, const void* Kc, const void* Vc, const uint8_t* ks, const uint8_t* vs, const int32_t* table) {
+  if (!aligned_to(Kc, 16) || !aligned_to(Vc, 16) || !aligned_to(table, 4)) return SPT_ERR_ARG;
+  const bool e4m3 = s.format == SPT_CACHE_E4M3;
+  if (e4m3 ? (!aligned_to(ks, 16) || !aligned_to(vs, 16)) : (ks || vs)) return SPT_ERR_ARG;
+  return SPT_OK;
+}
+
+CacheArgs cache_args(const spt_cache_shape_t& s, const void* Kc, const void* Vc, const uint8_t* ks, const uint8_t* vs, const int32_t* table) {
+  return {const_cast<char*>(static_cast<const char*>(Kc)), const_cast<char*>(static_cast<const char*>(Vc)), const_cast<uint8_t*>(ks),
+          const_cast<uint8_t*>(vs), table, s.pages, __builtin_ctz(s.page), s.Hk, s.B, s.max_pages};
+}
+
+int check_rows(const spt_cache_shape_t* s, int32_t T, const void* K, const void* V, const int64_t* strides, const int32_t* start, const int32_t* cu,
+               bool output, RowArgs* a) {
+  int rc = check_cache(s);
+  if (rc != SPT_OK) return rc;
+  if (T < 1) return SPT_ERR_ARG;
+  if ((rc = attn_rows(&a->K, K, strides, T, s->Hk, s->dh, output)) != SPT_OK) return rc;
+  if ((rc = attn_rows(&a->V, V, strides ? strides + 2 : nullptr, T, s->Hk, s->dh, output)) != SPT_OK) return rc;
+  if (!aligned_to(start, 4) || !aligned_to(cu, 4)) return SPT_ERR_ARG;
+  a->start = start; a->cu = cu; a->T = T;
+  return SPT_OK;
+}
+
+// Workgroups of the decoding launch: as many as are resident at once.
+int decode_workgroups(const spt_cache_shape_t& s) {
+  const int row = s.format == SPT_CACHE_E4M3 ? s.dh : 2 * s.dh;
+  return 256 * (row == 256 ? 1 : row == 128 ? 2 : 4);
+}
+
+struct DecodeWorkspace { int sets, rows; size_t part, bytes; };
+DecodeWorkspace plan_decode(const spt_cache_shape_t& s, int H) {
+  const int G = H / s.Hk, rows = G < 16 ? G : 16;
+  const size_t slots = 2 * (size_t)decode_workgroups(s) * rows;
+  const size_t part = align256(slots * s.dh * sizeof(float));
+  return {(G + 15) / 16, rows, part, part + align256(slots * 2 * sizeof(float))};
+}
+
+int check_decode(const spt_cache_shape_t* s, int32_t H) {
+  const int rc = check_cache(s);
+  if (rc != SPT_OK) return rc;
+  if (H < 1 || H % s->Hk != 0) return SPT_ERR_ARG;
+  if (H > 65535) return SPT_ERR_UNSUPPORTED;
+  const int64_t units = ((int64_t)s->max_pages * s->page + kUnit - 1) / kUnit * s->Hk * ((H / s->Hk + 15) / 16);
+  if (units > INT_MAX || units * s->B > INT_MAX || (int64_t)s->B * H > INT_MAX) return SPT_ERR_UNSUPPORTED;
+  return SPT_OK;
+}
+
+template <int DH, bool E4M3>
+hipError_t launch_decode(const DecodeArgs& a, hipStream_t st) {
+  typedef DecodeTile<DH, E4M3> T;
+  constexpr int join = kDecodeWaves * 16 * (2 + DH + 4) * 4, smem = kDecodeWaves * T::RING > join ? kDecodeWaves * T::RING : join;
+  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(decode_kernel<DH, E4M3>), hipFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (e != hipSuccess) return e;
+  {
+    ScopedKernelTimer timer(kSlotAttnDecode, st);
+    hipLaunchKernelGGL((decode_kernel<DH, E4M3>), dim3(a.workgroups), dim3(64 * kDecodeWaves), smem, st, a);
+  }
+  if (const hipError_t e2 = hipGetLastError(); e2 != hipSuccess) return e2;
+  ScopedKernelTimer timer(kSlotAttnDecodeJoin, st);
+  hipLaunchKernelGGL(decode_join_kernel<DH>, dim3((a.c.B * a.H + 3) / 4), dim3(256), 0, st, a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+extern "C" int spt_cache_write(const spt_cache_shape_t* shape, int32_t T, const void* K, const void* V, const int64_t* strides,
+                               const int32_t* table, const int32_t* start, const int32_t* cu, void* Kc, void* Vc, uint8_t* ks, uint8_t* vs,
+                               void* stream) {
+  RowArgs a;
+  int rc = check_rows(shape, T, K, V, strides, start, cu, false, &a);
+  if (rc != SPT_OK) return rc;
+  if ((rc = check_pool(*shape, Kc, Vc, ks, vs, table)) != SPT_OK) return rc;
+  a.c = cache_args(*shape, Kc, Vc, ks, vs, table);
+  const hipStream_t st = static_cast<hipStream_t>(stream);
+  ScopedKernelTimer timer(kSlotCacheWrite, st);
+  const dim3 grid((T + 3) / 4), block(256);
+  const bool e4m3 = shape->format == SPT_CACHE_E4M3;
+  if (shape->dh == 128 && e4m3) hipLaunchKernelGGL((cache_write_kernel<128, true>), grid, block, 0, st, a);
+  else if (shape->dh == 128) hipLaunchKernelGGL((cache_write_kernel<128, false>), grid, block, 0, st, a);
+  else if (e4m3) hipLaunchKernelGGL((cache_write_kernel<64, true>), grid, block, 0, st, a);
+  else hipLaunchKernelGGL((cache_write_kernel<64, false>), grid, block, 0, st, a);
+  return hipGetLastError() == hipSuccess ? SPT_OK : SPT_ERR_HIP;
+}
+
+extern "C" int spt_cache_read(const spt_cache_shape_t* shape, int32_t T, void* K, void* V, const int64_t* strides, const int32_t* table,
+                              const int32_t* start, const int32_t* cu, const void* Kc, const void* Vc, const uint8_t* ks,
+                              const uint8_t* vs, void* stream) {
+  RowArgs a;
+  int rc = check_rows(shape, T, K, V, strides, start, cu, true, &a);
+  if (rc != SPT_OK) return rc;
+  if ((rc = check_pool(*shape, Kc, Vc, ks, vs, table)) != SPT_OK) return rc;
+  a.c = cache_args(*shape, Kc, Vc, ks, vs, table);
+  const hipStream_t st = static_cast<hipStream_t>(stream);
+  ScopedKernelTimer timer(kSlotCacheRead, st);
+  const dim3 grid((T + 3) / 4), block(256);
+  const bool e4m3 = shape->format == SPT_CACHE_E4M3;
+  if (shape->dh == 128 && e4m3) hipLaunchKernelGGL((cache_read_kernel<128, true>), grid, block, 0, st, a);
+  else if (shape->dh == 128) hipLaunchKernelGGL((cache_read_kernel<128, false>), grid, block, 0, st, a);
+  else if (e4m3) hipLaunchKernelGGL((cache_read_kernel<64, true>), grid, block, 0, st, a);
+  else hipLaunchKernelGGL((cache_read_kernel<64, false>), grid, block, 0, st, a);
+  return hipGetLastError() == hipSuccess ? SPT_OK : SPT_ERR_HIP;
+}
+
+extern "C" size_t spt_attn_decode_workspace_bytes(const spt_cache_shape_t* shape, int32_t H) {
+  if (check_decode(shape, H) != SPT_OK) return 0;
+  return plan_decode(*shape, H).bytes;
+}
+
+extern "C" int spt_attn_decode(const spt_cache_shape_t* shape, int32_t H, float scale, const void* Q, const int64_t* strides, const void* Kc,
+                               const void* Vc, const uint8_t* ks, const uint8_t* vs, const int32_t* table, const int32_t* lens, void* Y,
+                               void* ws, size_t ws_bytes, void* stream) {
+  int rc = check_decode(shape, H);
+  if (rc != SPT_OK) return rc;
+  if (!isfinite(scale) || !(scale > 0.f)) return SPT_ERR_ARG;
+  const spt_cache_shape_t& s = *shape;
+  DecodeArgs a;
+  if ((rc = attn_rows(&a.Q, Q, strides, s.B, H, s.dh, false)) != SPT_OK) return rc;
+  if ((rc = attn_rows(&a.Y, Y, strides ? strides + 2 : nullptr, s.B, H, s.dh, true)) != SPT_OK) return rc;
+  if ((rc = check_pool(s, Kc, Vc, ks, vs, table)) != SPT_OK) return rc;
+  if (!aligned_to(lens, 4) || !aligned_to(ws, 256)) return SPT_ERR_ARG;
+  const DecodeWorkspace w = plan_decode(s, H);
+  if (ws_bytes < w.bytes) return SPT_ERR_WORKSPACE;
+  a.c = cache_args(s, Kc, Vc, ks, vs, table);
+  a.lens = lens;
+  a.part = static_cast<float*>(ws);
+  a.stat = reinterpret_cast<float*>(static_cast<char*>(ws) + w.part);
+  a.H = H; a.G = H / s.Hk; a.sets = w.sets; a.rows = w.rows;
+  a.workgroups = decode_workgroups(s);
+  a.cs = scale * kLog2e;
+  const hipStream_t st = static_cast<hipStream_t>(stream);
+  const bool e4m3 = s.format == SPT_CACHE_E4M3;
+  const hipError_t e = s.dh == 128 ? (e4m3 ? launch_decode<128, true>(a, st) : launch_decode<128, false>(a, st))
+                                   : (e4m3 ? launch_decode<64, true>(a, st) : launch_decode<64, false>(a, st));
+  return e == hipSuccess ? SPT_OK : SPT_ERR_HIP;
+}

@@ -1,0 +1,171 @@
+// What the kernels of full attention share (attn_prompt.hip, attn_prompt_bwd.hip, attn_cache.hip): row tiles in
+// LDS, the search for a workgroup's sequence, checks of arguments.  gfx950 only.
+#pragma once
+#include <limits.h>
+#include <math.h>
+
+#include "../../include/spt_attn.h"
+#include "ffn_common.hpp"
+#include "profile.hpp"
+#include "spt_host.hpp"
+
+namespace spt {
+
+// A tensor of rows [T][heads][dh] bf16, with the bytes from a row to the next and from a head to the next.
+struct AttnRows {
+  char* p;
+  int64_t row, head;
+};
+
+// ---- host side
+
+inline bool aligned_to(const void* p, size_t a) { return p && (reinterpret_cast<uintptr_t>(p) % a) == 0; }
+
+// Rows T, heads, of a tensor at p; strides: its two numbers or null (dense).  An output's rows and heads must not overlap.
+inline int attn_rows(AttnRows* r, const void* p, const int64_t* strides, int64_t T, int heads, int dh, bool output) {
+  if (!aligned_to(p, 16)) return SPT_ERR_ARG;
+  const int64_t row = strides ? strides[0] : (int64_t)heads * dh, head = strides ? strides[1] : dh;
+  if (row < 0 || head < 0 || row % 8 != 0 || head % 8 != 0) return SPT_ERR_ARG;
+  if (row >= (1 << 23) || head >= (1 << 23)) return strides ? SPT_ERR_UNSUPPORTED : SPT_ERR_ARG;
+  if (output) {
+    const bool rows_in_head = heads == 1 || head >= (T - 1) * row + dh, heads_in_row = T == 1 || row >= (heads - 1) * head + dh;
+    if ((T > 1 && row < dh) || (heads > 1 && head < dh) || (!rows_in_head && !heads_in_row)) return SPT_ERR_ARG;
+  }
+  *r = AttnRows{const_cast<char*>(static_cast<const char*>(p)), row * 2, head * 2};
+  return SPT_OK;
+}
+
+int check_attn(const spt_attn_shape_t* s);   // attn_prompt.hip
+int attn_heads_shift(int G);                // log2 of the heads of a group of G that share a workgroup
+
+// ---- device side
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+// A word at an address that all lanes share, through the scalar cache: vector memory's counter, which the copies into
+// LDS are waited for by, does not see it.
+__device__ __forceinline__ int32_t uniform_load(const int32_t* p) {
+  return *reinterpret_cast<const __attribute__((address_space(4))) int32_t*>(reinterpret_cast<uintptr_t>(p));
+}
+
+// A sequence's rows of a packed tensor.
+struct SeqRows { int first, n; };
+__device__ __forceinline__ SeqRows seq_rows(const int32_t* cu, int b, int T) {
+  const int lo = min(max(cu[b], 0), T), hi = min(max(cu[b + 1], 0), T);
+  return {lo, max(0, hi - lo)};
+}
+
+// Tile t of all sequences' row tiles of `rows` rows, in order: its sequence and the tile's number in it.  All lanes of a
+// wavefront look together, 64 sequences at a time.  False: there are not so many tiles.
+__device__ __forceinline__ bool find_tile(const int32_t* cu, int B, int T, int rows_shift, int t, int& b, int& tile, SeqRows& s) {
+  const int lane = threadIdx.x & 63;
+  int before = 0;
+  for (int b0 = 0; b0 < B; b0 += 64) {
+    const int mine = b0 + lane;
+    SeqRows x = {0, 0};
+    if (mine < B) x = seq_rows(cu, mine, T);
+    int incl = (x.n + (1 << rows_shift) - 1) >> rows_shift;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int up = __shfl_up(incl, o);
+      if (lane >= o) incl += up;
+    }
+    const int total = __builtin_amdgcn_readlane(incl, 63);
+    if (t - before < total) {
+      const int src = __builtin_ctzll(__ballot(incl > t - before));
+      b = b0 + src;
+      s = {__builtin_amdgcn_readlane(x.first, src), __builtin_amdgcn_readlane(x.n, src)};
+      tile = t - before - (src > 0 ? __builtin_amdgcn_readlane(incl, src - 1) : 0);
+      return true;
+    }
+    before += total;
+  }
+  return false;
+}
+
+// Workgroup id -> place in a list that the eight XCDs (workgroup id mod 8) share in contiguous parts.
+__device__ __forceinline__ int xcd_contiguous(int id, int total) {
+  const int q = total >> 3, r = total & 7, x = id & 7;
+  return x * q + min(x, r) + (id >> 3);
+}
+
+// 16-byte chunk of a tile of rows of RB bytes in LDS: chunk c of row r sits at c ^ chunk_swizzle(r).  Sixteen rows at one
+// chunk (an MFMA operand's reads), four rows at four adjacent chunks and eight rows at two (transposing reads) all reach all banks.
+template <int RB>
+__device__ __forceinline__ uint32_t chunk_swizzle(int r) {
+  const uint32_t low = ((r >> 1) & 2) | ((r >> 3) & 1);   // bits 2 and 3 of r
+  return RB == 256 ? (uint32_t)((r & 3) << 2) | low : RB == 128 ? (uint32_t)(((r >> 1) & 1) << 2) | low : low;
+}
+template <int DH>
+__device__ __forceinline__ uint32_t row_swizzle(int r) { return chunk_swizzle<DH * 2>(r); }
+
+// Asynchronous copy global -> LDS, 16 (4) bytes per lane from base + off; lane L's data lands at lds_base + 16 L (4 L).
+__device__ __forceinline__ void dma16_at(const void* base, uint32_t off, uint32_t lds_base) {
+  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds_base), "v"(off), "s"(base) : "memory");
+}
+__device__ __forceinline__ void dma4_at(const void* base, uint32_t off, uint32_t lds_base) {
+  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds_base), "v"(off), "s"(base) : "memory");
+}
+__device__ __forceinline__ uint32_t lds_addr(const void* p) { return __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)p); }
+
+// Fragment reads of a row tile.  row_frag: 8 dims (16 ks + 8 h ..) of row `row`, the operand whose K is the head dimension;
+// `base` = the lane's row_frag_base.  col_frag: 4 + 4 rows of one dim, the operand whose K are the rows.
+template <int DH>
+__device__ __forceinline__ bf16x8 row_frag(const char* tile, int row, int ks, int h) {
+  return *reinterpret_cast<const bf16x8*>(tile + row * (DH * 2) + (((uint32_t)(2 * ks + h) ^ row_swizzle<DH>(row)) * 16));
+}
+// Transposed operand of 32 dims (dt) x 16 rows (row0 ..): MFMA row i is dim 32 dt + rho32(i), so that a lane's 16 results are
+// adjacent dims; K slot (h, e) is row row0 + 8 (e / 4) + 4 h + e % 4, the order in which a lane holds the results
+// of a product whose rows are these.
+template <int DH>
+__device__ __forceinline__ bf16x8 col_frag(const char* tile, int row0, int dt, int lane) {
+  const int g = lane >> 4, sl = lane & 15, a4 = sl & 3;
+  const int row = row0 + 4 * (g >> 1) + (sl >> 2);
+  const uint32_t chunk = dt * 4 + 2 * (a4 & 1) + (g & 1);
+  const char* lo = tile + row * (DH * 2) + (chunk ^ row_swizzle<DH>(row)) * 16 + (a4 >> 1) * 8;
+  const char* hi = tile + (row + 8) * (DH * 2) + (chunk ^ row_swizzle<DH>(row + 8)) * 16 + (a4 >> 1) * 8;
+  return tr_read_frag(lo, hi);
+}
+
+__device__ __forceinline__ float other_half(float x) {   // the value of the lane 32 away
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float((threadIdx.x & 32) ? r[0] : r[1]);
+}
+
+// Eight fp32 -> an MFMA operand, nearest even.
+__device__ __forceinline__ bf16x8 pack8(const float* x) {
+  return as_bf16x8(u32x4{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7])});
+}
+
+// Whether one of eight bf16 is infinite or NaN.
+__device__ __forceinline__ bool any_not_finite(u32x4 x) {
+  bool bad = false;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) bad |= (x[e] & 0x7F80u) == 0x7F80u || (x[e] & 0x7F800000u) == 0x7F800000u;
+  return bad;
+}
+
+__device__ __forceinline__ float wave_sum(float x) {
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) x += __shfl_xor(x, o);
+  return x;
+}
+__device__ __forceinline__ float wave_max(float x) {
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) x = fmaxf(x, __shfl_xor(x, o));
+  return x;
+}
+
+// dot product of two rows of dh values, one lane's.
+__device__ __forceinline__ float row_dot(const char* a, const char* b, int dh) {
+  float s = 0.f;
+  for (int c = 0; c < dh; c += 8) {
+    const u32x4 x = *reinterpret_cast<const u32x4*>(a + c * 2), y = *reinterpret_cast<const u32x4*>(b + c * 2);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) s = fmaf(hi_bf16(x[e]), hi_bf16(y[e]), fmaf(lo_bf16(x[e]), lo_bf16(y[e]), s));
+  }
+  return s;
+}
+__device__ __forceinline__ float bf16_at(const char* p) { return bf16_to_f32(*reinterpret_cast<const uint16_t*>(p)); }
+
+}  // namespace spt

@@ -1,0 +1,248 @@
+// Full attention over packed sequences, forward (include/spt_attn.h).
+//
+// A workgroup of four wavefronts owns 128 query rows: 128 / HW positions of one sequence times HW heads that
+// share a key head (HW: 4, 2 or 1, as divides the group).  A wavefront owns 32 of them.  Keys and values pass through LDS in
+// tiles of 64, copied asynchronously one tile ahead.  Scores are formed transposed, S^T = K Q^T, so that a lane holds 16
+// scores of ONE query and half of them are what the second product's operand wants of it: P stays in registers, and
+// maximum, sum and rescaling of a query are one lane's (two halves of a row meet in one lane swap).  O^T = V^T P^T takes V out of LDS
+// through the transposing read.  One pass over the keys: running maximum m and sum l, p = 2^(c s - m) with c = scale log2 e; the
+// accumulators are rescaled only when a maximum rises by more than 2^8 (p stays below 256, and the sums are fp32).
+#include "attn_common.hpp"
+
+using namespace spt;
+
+namespace {
+
+constexpr int kTileKeys = 64;
+constexpr float kLazy = 8.f;   // a row's maximum may be this much (log2) above what its sums are scaled by
+
+struct FwdArgs {
+  AttnRows Q, K, V, Y;
+  const int32_t *cu_q, *cu_k;
+  float* lse;
+  int B, Tq, Tk, Hk, G, hshift;   // G = H / Hk, 1 << hshift heads of a group in a workgroup
+  int tiles, units;               // tiles of positions at most, workgroups
+  int causal;
+  float c;
+};
+
+// A row the plain way, for wavefronts that met infinities or NaN in rows that some of their queries must not see: lanes
+// take keys for the scores, dims for the sum, and only the `n` visible keys are touched.
+template <int DH>
+__device__ __forceinline__ void slow_row(const char* q, const char* k, int64_t kstep, const char* v, int64_t vstep, int n, float c, char* y,
+                                         float* lse) {
+  const int lane = threadIdx.x & 63;
+  float m = -INFINITY, l = 0.f, acc[DH / 64] = {};
+  for (int j0 = 0; j0 < n; j0 += 64) {
+    const int j = j0 + lane;
+    const float t = j < n ? row_dot(q, k + j * kstep, DH) * c : -INFINITY;
+    const float mn = fmaxf(m, wave_max(t)), ms = mn == -INFINITY ? 0.f : mn;
+    const float p = j < n ? __builtin_amdgcn_exp2f(t - ms) : 0.f, alpha = __builtin_amdgcn_exp2f(m - ms);
+    m = mn;
+    l = l * alpha + wave_sum(p);
+#pragma unroll
+    for (int d = 0; d < DH / 64; ++d) acc[d] *= alpha;
+    for (int e = 0; e < min(64, n - j0); ++e) {
+      const float w = __shfl(p, e);
+#pragma unroll
+      for (int d = 0; d < DH / 64; ++d) acc[d] = fmaf(w, bf16_at(v + (j0 + e) * vstep + (lane + 64 * d) * 2), acc[d]);
+    }
+  }
+#pragma unroll
+  for (int d = 0; d < DH / 64; ++d)
+    reinterpret_cast<uint16_t*>(y)[lane + 64 * d] = (uint16_t)pack_bf16x2(l == 0.f ? 0.f : acc[d] / l, 0.f);
+  if (lse && lane == 0) *lse = (m + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
+template <int DH>
+__global__ __launch_bounds__(256, 2) void prompt_fwd_kernel(const FwdArgs a) {
+  constexpr int KS = DH / 16, DT = DH / 32, TILE_BYTES = kTileKeys * DH * 2;
+  __shared__ __align__(256) char smem[4 * TILE_BYTES];   // K, V, twice
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 31, h = lane >> 5;
+
+  const int hsets = a.G >> a.hshift, unit = xcd_contiguous(blockIdx.x, a.units);
+  const int hk = unit / (hsets * a.tiles), rest = unit - hk * (hsets * a.tiles);
+  // (the tiles that see the most keys first)
+  const int t_all = a.tiles - 1 - rest / hsets, hs = rest % hsets;
+  const int pshift = 7 - a.hshift;                       // positions of a workgroup
+  int b, tile;
+  SeqRows sq;
+  if (!find_tile(a.cu_q, a.B, a.Tq, pshift, t_all, b, tile, sq)) return;
+  const SeqRows sk = seq_rows(a.cu_k, b, a.Tk);
+  const int nq = sq.n, nk = sk.n, ahead = nk - nq;       // query i sees keys up to i + ahead
+  const int head = hk * a.G + (hs << a.hshift) + (wave & ((1 << a.hshift) - 1));
+  const int p0 = (tile << pshift), i0 = p0 + (wave >> a.hshift) * 32;
+  const int last = min(nq, p0 + (1 << pshift)) - 1;
+  const int kend = a.causal ? min(nk, last + ahead + 1) : nk;            // keys that the workgroup sees any of
+  const int wave_kend = i0 >= nq ? 0 : a.causal ? min(nk, min(nq, i0 + 32) + ahead) : nk;
+  const int wave_full = i0 >= nq ? 0 : a.causal ? min(nk, i0 + ahead + 1) : nk;   // ... that all queries of the wavefront see
+  const int mine = min(i0 + i, nq - 1);
+  const int seen = a.causal ? min(nk, mine + ahead + 1) : nk;            // keys the lane's query sees (may be negative)
+  const int ntile = kend > 0 ? (kend + kTileKeys - 1) / kTileKeys : 0;
+
+  const char* qrow = a.Q.p + (int64_t)(sq.first + mine) * a.Q.row + (int64_t)head * a.Q.head;
+  bf16x8 qf[KS];
+#pragma unroll
+  for (int s = 0; s < KS; ++s) qf[s] = *reinterpret_cast<const bf16x8*>(qrow + s * 32 + h * 16);
+
+  const char* kbase = a.K.p + (int64_t)sk.first * a.K.row + (int64_t)hk * a.K.head;
+  const char* vbase = a.V.p + (int64_t)sk.first * a.V.row + (int64_t)hk * a.V.head;
+  // copies: lane L of an instruction fills 16 bytes of row (u 256 + tid) / (DH / 8)
+  constexpr int COPIES = kTileKeys * (DH / 8) / 256;
+  auto fetch = [&](int t, int buf) {
+    const int j0 = t * kTileKeys;
+    const char* kb = kbase + (int64_t)j0 * a.K.row;
+    const char* vb = vbase + (int64_t)j0 * a.V.row;
+#pragma unroll
+    for (int u = 0; u < COPIES; ++u) {
+      const int slot = u * 256 + (int)threadIdx.x, row = slot / (DH / 8);
+      const uint32_t chunk = ((slot % (DH / 8)) ^ row_swizzle<DH>(row)) * 16;
+      const uint32_t r = (uint32_t)min(row, nk - 1 - j0);               // (rows past the end: the last one again)
+      const uint32_t at = lds_addr(smem + buf * 2 * TILE_BYTES + u * 4096 + wave * 1024);
+      dma16_at(kb, r * (uint32_t)a.K.row + chunk, at);
+      dma16_at(vb, r * (uint32_t)a.V.row + chunk, at + TILE_BYTES);
+    }
+  };
+  f32x16 o[DT];
+#pragma unroll
+  for (int d = 0; d < DT; ++d)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[d][r] = 0.f;
+  float m = -INFINITY, neg_m = 0.f, l = 0.f;
+  bool bad = false;
+
+  if (ntile > 0) fetch(0, 0);
+  for (int t = 0; t < ntile; ++t) {
+    wait_vmcnt<0>();
+    __syncthreads();
+    if (t + 1 < ntile) fetch(t + 1, (t + 1) & 1);
+    const int j0 = t * kTileKeys;
+    if (j0 >= wave_kend) continue;
+    const char* kt_ = smem + (t & 1) * 2 * TILE_BYTES;
+    const char* vt_ = kt_ + TILE_BYTES;
+    f32x16 s[2];
+#pragma unroll
+    for (int kt = 0; kt < 2; ++kt) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[kt][r] = 0.f;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks)
+        s[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(row_frag<DH>(kt_, 32 * kt + i, ks, h), qf[ks], s[kt], 0, 0, 0);
+    }
+    if (j0 + kTileKeys > wave_full) {
+      const int left = seen - j0 - 4 * h;
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[kt][r] = 32 * kt + 8 * (r >> 2) + (r & 3) < left ? s[kt][r] : -INFINITY;
+      // rows of V that some query must not see: 0 times an infinity is NaN
+#pragma unroll
+      for (int u = 0; u < TILE_BYTES / 1024; ++u) bad |= any_not_finite(*reinterpret_cast<const u32x4*>(vt_ + u * 1024 + lane * 16));
+    }
+    float top = s[0][0];
+#pragma unroll
+    for (int r = 1; r < 32; ++r) top = fmaxf(top, s[r >> 4][r & 15]);
+    top = fmaxf(top, other_half(top)) * a.c;
+    if (__any(top > m + kLazy)) {
+      const float mn = fmaxf(m, top), ms = mn == -INFINITY ? 0.f : mn;
+      const float alpha = __builtin_amdgcn_exp2f(m - ms);
+      m = mn;
+      neg_m = -ms;
+      l *= alpha;
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[d][r] *= alpha;
+    }
+    bf16x8 pf[2][2];
+#pragma unroll
+    for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        float p[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          p[e] = __builtin_amdgcn_exp2f(fmaf(s[kt][8 * half + e], a.c, neg_m));
+          l += p[e];
+        }
+        pf[kt][half] = pack8(p);
+      }
+#pragma unroll
+    for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+      for (int half = 0; half < 2; ++half)
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(col_frag<DH>(vt_, 32 * kt + 16 * half, d, lane), pf[kt][half], o[d], 0, 0, 0);
+  }
+
+  float* lse = a.lse ? a.lse + (int64_t)head * a.Tq + sq.first : nullptr;
+  if (__any(bad)) {
+    for (int r = 0; r < min(32, nq - i0); ++r) {
+      const int row = i0 + r;
+      slow_row<DH>(a.Q.p + (int64_t)(sq.first + row) * a.Q.row + (int64_t)head * a.Q.head, kbase, a.K.row, vbase, a.V.row,
+                   a.causal ? min(nk, row + ahead + 1) : nk, a.c, a.Y.p + (int64_t)(sq.first + row) * a.Y.row + (int64_t)head * a.Y.head,
+                   lse ? lse + row : nullptr);
+    }
+    return;
+  }
+  if (i0 + i >= nq) return;
+  l += other_half(l);
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  char* y = a.Y.p + (int64_t)(sq.first + mine) * a.Y.row + (int64_t)head * a.Y.head + h * 32;
+#pragma unroll
+  for (int d = 0; d < DT; ++d) {
+    float v[16];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) v[r] = o[d][r] * inv;
+    *reinterpret_cast<bf16x8*>(y + d * 64) = pack8(v);
+    *reinterpret_cast<bf16x8*>(y + d * 64 + 16) = pack8(v + 8);
+  }
+  if (lse && h == 0) lse[mine] = (m + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
+}  // namespace
+
+namespace spt {
+
+int check_attn(const spt_attn_shape_t* s) {
+  if (!s) return SPT_ERR_ARG;
+  if (s->B < 1 || s->Tq < 1 || s->Tk < 1 || s->H < 1 || s->Hk < 1 || s->dh < 1 || s->H % s->Hk != 0) return SPT_ERR_ARG;
+  if (s->causal != 0 && s->causal != 1) return SPT_ERR_ARG;
+  if (!isfinite(s->scale) || !(s->scale > 0.f)) return SPT_ERR_ARG;
+  if ((s->dh != 64 && s->dh != 128) || s->B > 65535 || s->H > 65535) return SPT_ERR_UNSUPPORTED;
+  // (workgroups: tiles of 32 rows at least, in every sequence, times heads)
+  if (((int64_t)s->Tq / 32 + s->B) * s->H > INT_MAX || ((int64_t)s->Tk / 32 + s->B) * s->H > INT_MAX) return SPT_ERR_UNSUPPORTED;
+  return SPT_OK;
+}
+
+int attn_heads_shift(int G) { return G % 4 == 0 ? 2 : G % 2 == 0 ? 1 : 0; }
+
+}  // namespace spt
+
+extern "C" int spt_attn_prompt_fwd(const spt_attn_shape_t* shape, const void* Q, const void* K, const void* V,
+                                   const int64_t* strides, const int32_t* cu_q, const int32_t* cu_k, void* Y, float* lse,
+                                   void* stream) {
+  int rc = check_attn(shape);
+  if (rc != SPT_OK) return rc;
+  const spt_attn_shape_t& s = *shape;
+  FwdArgs a;
+  auto at = [&](int n) { return strides ? strides + 2 * n : nullptr; };
+  if ((rc = attn_rows(&a.Q, Q, at(0), s.Tq, s.H, s.dh, false)) != SPT_OK) return rc;
+  if ((rc = attn_rows(&a.K, K, at(1), s.Tk, s.Hk, s.dh, false)) != SPT_OK) return rc;
+  if ((rc = attn_rows(&a.V, V, at(2), s.Tk, s.Hk, s.dh, false)) != SPT_OK) return rc;
+  if ((rc = attn_rows(&a.Y, Y, at(3), s.Tq, s.H, s.dh, true)) != SPT_OK) return rc;
+  if (!aligned_to(cu_q, 4) || !aligned_to(cu_k, 4) || (lse && !aligned_to(lse, 4))) return SPT_ERR_ARG;
+  a.cu_q = cu_q; a.cu_k = cu_k; a.lse = lse;
+  a.B = s.B; a.Tq = s.Tq; a.Tk = s.Tk; a.Hk = s.Hk; a.G = s.H / s.Hk;
+  a.hshift = attn_heads_shift(a.G);
+  a.tiles = (int)(((int64_t)s.Tq >> (7 - a.hshift)) + s.B);
+  a.units = a.tiles * s.Hk * (a.G >> a.hshift);
+  a.causal = s.causal;
+  a.c = s.scale * kLog2e;
+  const hipStream_t st = static_cast<hipStream_t>(stream);
+  ScopedKernelTimer timer(kSlotAttnFwd, st);
+  if (s.dh == 128) hipLaunchKernelGGL(prompt_fwd_kernel<128>, dim3(a.units), dim3(256), 0, st, a);
+  else hipLaunchKernelGGL(prompt_fwd_kernel<64>, dim3(a.units), dim3(256), 0, st, a);
+  return hipGetLastError() == hipSuccess ? SPT_OK : SPT_ERR_HIP;
+}

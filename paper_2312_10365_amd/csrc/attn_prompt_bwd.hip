@@ -1,0 +1,413 @@
+// Full attention over packed sequences, backward (include/spt_attn.h): two launches, both without atomics.
+//
+//   prompt_bwd_q_kernel   the forward's decomposition (a wavefront owns 32 query rows, keys pass through LDS): S^T and dP^T as products
+//                         with the query side in registers, dS^T in registers, dQ^T += K^T dS^T.  D = dy.y comes from a Y that was rounded to bf16 and
+//                         computed with weights that were, and where one key has nearly all the weight dS is what is left of dP - D
+//                         when they cancel.  The sum of a row's dS, 0 but for that, says by how much D is off: dq gets
+//                         that times sum_j p_j k_j (a product more on operands that are there) taken off, and the second
+//                         launch gets the corrected D.  Without it dQ and dK were 5e-3 off (2-norm, queries that prefer a key; 32 heads of 64,
+//                         512 tokens), with it 2.4e-3.
+//   prompt_bwd_kv_kernel  a wavefront owns 32 keys of a key head, the queries of all heads of its group pass through LDS in tiles
+//                         of 32, heads outermost, so a gradient is summed in one fixed order: S and dP with the key side in
+//                         registers, dV^T += dY^T P, dK^T += Q^T dS.
+// S and dP are formed in both: the alternative, keeping dS or partial dQ in memory, moves as many bytes as it saves time.
+#include "attn_common.hpp"
+
+using namespace spt;
+
+namespace {
+
+constexpr int kTileKeys = 64, kTileQueries = 32, kOwnKeys = 128;
+
+struct BwdArgs {
+  AttnRows Q, K, V, Y, dY, dQ, dK, dV;
+  const int32_t *cu_q, *cu_k;
+  const float* lse;
+  float* D;                       // [H][Tq]
+  int B, Tq, Tk, Hk, G, hshift;
+  int tiles, units;               // of the launch
+  int causal;
+  float c, scale;
+};
+
+// exp2 argument's subtrahend of a row: rows without a key have lse = -inf and p = 0
+__device__ __forceinline__ float row_offset(float lse) { return lse == -INFINITY ? INFINITY : lse * kLog2e; }
+
+// p and dS of one pair, from its rows in memory.
+struct PairGrad { float p, ds; };
+__device__ __forceinline__ PairGrad pair_grad(const char* q, const char* k, const char* dy, const char* v, int dh, float c, float off, float D) {
+  const float p = __builtin_amdgcn_exp2f(fmaf(row_dot(q, k, dh), c, -off));
+  return {p, p * (row_dot(dy, v, dh) - D)};
+}
+
+template <int DH>
+__device__ __forceinline__ void slow_dq_row(const BwdArgs& a, const char* q, const char* dy, const char* k, const char* v, int n, float off,
+                                            float D, char* dq) {
+  const int lane = threadIdx.x & 63;
+  float acc[DH / 64] = {};
+  for (int j0 = 0; j0 < n; j0 += 64) {
+    const int j = j0 + lane;
+    const float ds = j < n ? pair_grad(q, k + j * a.K.row, dy, v + j * a.V.row, DH, a.c, off, D).ds : 0.f;
+    for (int e = 0; e < min(64, n - j0); ++e) {
+      const float w = __shfl(ds, e);
+#pragma unroll
+      for (int d = 0; d < DH / 64; ++d) acc[d] = fmaf(w, bf16_at(k + (j0 + e) * a.K.row + (lane + 64 * d) * 2), acc[d]);
+    }
+  }
+#pragma unroll
+  for (int d = 0; d < DH / 64; ++d) reinterpret_cast<uint16_t*>(dq)[lane + 64 * d] = (uint16_t)pack_bf16x2(acc[d] * a.scale, 0.f);
+}
+
+template <int DH>
+__global__ __launch_bounds__(256, DH == 128 ? 1 : 2) void prompt_bwd_q_kernel(const BwdArgs a) {
+  constexpr int KS = DH / 16, DT = DH / 32, TILE_BYTES = kTileKeys * DH * 2;
+  __shared__ __align__(256) char smem[4 * TILE_BYTES];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 31, h = lane >> 5;
+  const int hsets = a.G >> a.hshift, unit = xcd_contiguous(blockIdx.x, a.units);
+  const int hk = unit / (hsets * a.tiles), rest = unit - hk * (hsets * a.tiles);
+  const int t_all = a.tiles - 1 - rest / hsets, hs = rest % hsets;
+  const int pshift = 7 - a.hshift;
+  int b, tile;
+  SeqRows sq;
+  if (!find_tile(a.cu_q, a.B, a.Tq, pshift, t_all, b, tile, sq)) return;
+  const SeqRows sk = seq_rows(a.cu_k, b, a.Tk);
+  const int nq = sq.n, nk = sk.n, ahead = nk - nq;
+  const int head = hk * a.G + (hs << a.hshift) + (wave & ((1 << a.hshift) - 1));
+  const int p0 = (tile << pshift), i0 = p0 + (wave >> a.hshift) * 32;
+  const int last = min(nq, p0 + (1 << pshift)) - 1;
+  const int kend = a.causal ? min(nk, last + ahead + 1) : nk;
+  const int wave_kend = i0 >= nq ? 0 : a.causal ? min(nk, min(nq, i0 + 32) + ahead) : nk;
+  const int wave_full = i0 >= nq ? 0 : a.causal ? min(nk, i0 + ahead + 1) : nk;
+  const int mine = min(i0 + i, nq - 1);
+  const int seen = a.causal ? min(nk, mine + ahead + 1) : nk;
+  const int ntile = kend > 0 ? (kend + kTileKeys - 1) / kTileKeys : 0;
+
+  const int64_t row = sq.first + mine;
+  const char* qrow = a.Q.p + row * a.Q.row + (int64_t)head * a.Q.head;
+  const char* yrow = a.Y.p + row * a.Y.row + (int64_t)head * a.Y.head;
+  const char* dyrow = a.dY.p + row * a.dY.row + (int64_t)head * a.dY.head;
+  bf16x8 qf[KS], dyf[KS];
+  float D = 0.f;
+#pragma unroll
+  for (int s = 0; s < KS; ++s) {
+    qf[s] = *reinterpret_cast<const bf16x8*>(qrow + s * 32 + h * 16);
+    const u32x4 dy = *reinterpret_cast<const u32x4*>(dyrow + s * 32 + h * 16), y = *reinterpret_cast<const u32x4*>(yrow + s * 32 + h * 16);
+    dyf[s] = as_bf16x8(dy);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) D = fmaf(hi_bf16(dy[e]), hi_bf16(y[e]), fmaf(lo_bf16(dy[e]), lo_bf16(y[e]), D));
+  }
+  D += other_half(D);
+  const float off = row_offset(a.lse[(int64_t)head * a.Tq + row]);
+  const char* kbase = a.K.p + (int64_t)sk.first * a.K.row + (int64_t)hk * a.K.head;
+  const char* vbase = a.V.p + (int64_t)sk.first * a.V.row + (int64_t)hk * a.V.head;
+  constexpr int COPIES = kTileKeys * (DH / 8) / 256;
+  auto fetch = [&](int t, int buf) {
+    const int j0 = t * kTileKeys;
+    const char* kb = kbase + (int64_t)j0 * a.K.row;
+    const char* vb = vbase + (int64_t)j0 * a.V.row;
+#pragma unroll
+    for (int u = 0; u < COPIES; ++u) {
+      const int slot = u * 256 + (int)threadIdx.x, r0 = slot / (DH / 8);
+      const uint32_t chunk = ((slot % (DH / 8)) ^ row_swizzle<DH>(r0)) * 16;
+      const uint32_t r = (uint32_t)min(r0, nk - 1 - j0);
+      const uint32_t at = lds_addr(smem + buf * 2 * TILE_BYTES + u * 4096 + wave * 1024);
+      dma16_at(kb, r * (uint32_t)a.K.row + chunk, at);
+      dma16_at(vb, r * (uint32_t)a.V.row + chunk, at + TILE_BYTES);
+    }
+  };
+  f32x16 o[DT], mean[DT];                                // sums of dS k and of p k
+#pragma unroll
+  for (int d = 0; d < DT; ++d)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[d][r] = mean[d][r] = 0.f;
+  float left_over = 0.f;                                 // sum of dS: what D lacks
+  bool bad = false;
+
+  if (ntile > 0) fetch(0, 0);
+  for (int t = 0; t < ntile; ++t) {
+    wait_vmcnt<0>();
+    __syncthreads();
+    if (t + 1 < ntile) fetch(t + 1, (t + 1) & 1);
+    const int j0 = t * kTileKeys;
+    if (j0 >= wave_kend) continue;
+    const char* kt_ = smem + (t & 1) * 2 * TILE_BYTES;
+    const char* vt_ = kt_ + TILE_BYTES;
+    const bool masked = j0 + kTileKeys > wave_full;
+    if (masked) {
+#pragma unroll
+      for (int u = 0; u < TILE_BYTES / 1024; ++u) bad |= any_not_finite(*reinterpret_cast<const u32x4*>(kt_ + u * 1024 + lane * 16));
+    }
+#pragma unroll
+    for (int kt = 0; kt < 2; ++kt) {
+      f32x16 s, dp;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] = dp[r] = 0.f;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks)
+        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(row_frag<DH>(kt_, 32 * kt + i, ks, h), qf[ks], s, 0, 0, 0);
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks)
+        dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(row_frag<DH>(vt_, 32 * kt + i, ks, h), dyf[ks], dp, 0, 0, 0);
+      float p[16], ds[16];
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        p[r] = __builtin_amdgcn_exp2f(fmaf(s[r], a.c, -off));
+        ds[r] = p[r] * (dp[r] - D);
+      }
+      if (masked) {
+        const int left = seen - j0 - 32 * kt - 4 * h;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const bool sees = 8 * (r >> 2) + (r & 3) < left;
+          p[r] = sees ? p[r] : 0.f;
+          ds[r] = sees ? ds[r] : 0.f;
+        }
+      }
+#pragma unroll
+      for (int r = 0; r < 16; ++r) left_over += ds[r];
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        const bf16x8 pf = pack8(p + 8 * half), sf = pack8(ds + 8 * half);
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+          const bf16x8 f = col_frag<DH>(kt_, 32 * kt + 16 * half, d, lane);
+          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, sf, o[d], 0, 0, 0);
+          mean[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, pf, mean[d], 0, 0, 0);
+        }
+      }
+    }
+  }
+  float* Dout = a.D + (int64_t)head * a.Tq;
+  if (__any(bad)) {
+    for (int r = 0; r < min(32, nq - i0); ++r) {
+      const int64_t at = sq.first + i0 + r;
+      const float Dr = __shfl(D, r), offr = __shfl(off, r);
+      if (lane == 0) Dout[at] = Dr;
+      slow_dq_row<DH>(a, a.Q.p + at * a.Q.row + (int64_t)head * a.Q.head, a.dY.p + at * a.dY.row + (int64_t)head * a.dY.head, kbase, vbase,
+                      a.causal ? min(nk, i0 + r + ahead + 1) : nk, offr, Dr, a.dQ.p + at * a.dQ.row + (int64_t)head * a.dQ.head);
+    }
+    return;
+  }
+  if (i0 + i >= nq) return;
+  left_over += other_half(left_over);
+  if (h == 0) Dout[row] = D + left_over;
+  char* dq = a.dQ.p + row * a.dQ.row + (int64_t)head * a.dQ.head + h * 32;
+#pragma unroll
+  for (int d = 0; d < DT; ++d) {
+    float v[16];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) v[r] = fmaf(-left_over, mean[d][r], o[d][r]) * a.scale;
+    *reinterpret_cast<bf16x8*>(dq + d * 64) = pack8(v);
+    *reinterpret_cast<bf16x8*>(dq + d * 64 + 16) = pack8(v + 8);
+  }
+}
+
+// Both gradients of one key: lanes take queries for the pairs, dims for the sums.
+template <int DH>
+__device__ __forceinline__ void slow_dkv_row(const BwdArgs& a, const SeqRows& sq, int hk, int first, const char* k, const char* v, char* dk, char* dv) {
+  const int lane = threadIdx.x & 63;
+  float ak[DH / 64] = {}, av[DH / 64] = {};
+  for (int g = 0; g < a.G; ++g) {
+    const int head = hk * a.G + g;
+    const char* q = a.Q.p + (int64_t)sq.first * a.Q.row + (int64_t)head * a.Q.head;
+    const char* dy = a.dY.p + (int64_t)sq.first * a.dY.row + (int64_t)head * a.dY.head;
+    const int64_t stat = (int64_t)head * a.Tq + sq.first;
+    for (int i0 = first; i0 < sq.n; i0 += 64) {
+      const int i = i0 + lane;
+      PairGrad x = {0.f, 0.f};
+      if (i < sq.n) x = pair_grad(q + i * a.Q.row, k, dy + i * a.dY.row, v, DH, a.c, row_offset(a.lse[stat + i]), a.D[stat + i]);
+      for (int e = 0; e < min(64, sq.n - i0); ++e) {
+        const float p = __shfl(x.p, e), ds = __shfl(x.ds, e);
+#pragma unroll
+        for (int d = 0; d < DH / 64; ++d) {
+          av[d] = fmaf(p, bf16_at(dy + (i0 + e) * a.dY.row + (lane + 64 * d) * 2), av[d]);
+          ak[d] = fmaf(ds, bf16_at(q + (i0 + e) * a.Q.row + (lane + 64 * d) * 2), ak[d]);
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int d = 0; d < DH / 64; ++d) {
+    reinterpret_cast<uint16_t*>(dk)[lane + 64 * d] = (uint16_t)pack_bf16x2(ak[d] * a.scale, 0.f);
+    reinterpret_cast<uint16_t*>(dv)[lane + 64 * d] = (uint16_t)pack_bf16x2(av[d], 0.f);
+  }
+}
+
+template <int DH>
+__global__ __launch_bounds__(256, 1) void prompt_bwd_kv_kernel(const BwdArgs a) {
+  constexpr int KS = DH / 16, DT = DH / 32, TILE_BYTES = kTileQueries * DH * 2;
+  __shared__ __align__(256) char smem[4 * TILE_BYTES];    // Q, dY, twice
+  __shared__ __align__(256) float stat[2][64];            // lse, D of a tile's rows
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 31, h = lane >> 5;
+  const int unit = xcd_contiguous(blockIdx.x, a.units), hk = unit / a.tiles;
+  int b, tile;
+  SeqRows sk;
+  if (!find_tile(a.cu_k, a.B, a.Tk, 7, unit - hk * a.tiles, b, tile, sk)) return;
+  const SeqRows sq = seq_rows(a.cu_q, b, a.Tq);
+  const int nq = sq.n, nk = sk.n, ahead = nk - nq;
+  const int j0 = tile * kOwnKeys + wave * 32, mine = min(j0 + i, nk - 1);
+  const int first = a.causal ? max(0, mine - ahead) : 0;                 // the first query that sees the lane's key
+  const int begin = a.causal ? max(0, tile * kOwnKeys - ahead) & ~(kTileQueries - 1) : 0;
+  const int nt = begin < nq ? (nq - begin + kTileQueries - 1) / kTileQueries : 0, steps = nt * a.G;
+
+  const char* krow = a.K.p + (int64_t)(sk.first + mine) * a.K.row + (int64_t)hk * a.K.head;
+  const char* vrow = a.V.p + (int64_t)(sk.first + mine) * a.V.row + (int64_t)hk * a.V.head;
+  bf16x8 kf[KS], vf[KS];
+#pragma unroll
+  for (int s = 0; s < KS; ++s) {
+    kf[s] = *reinterpret_cast<const bf16x8*>(krow + s * 32 + h * 16);
+    vf[s] = *reinterpret_cast<const bf16x8*>(vrow + s * 32 + h * 16);
+  }
+  constexpr int COPIES = kTileQueries * (DH / 8) / 256;
+  auto fetch = [&](int g, int q0, int buf) {
+    const int head = hk * a.G + g;
+    const char* qb = a.Q.p + (int64_t)(sq.first + q0) * a.Q.row + (int64_t)head * a.Q.head;
+    const char* yb = a.dY.p + (int64_t)(sq.first + q0) * a.dY.row + (int64_t)head * a.dY.head;
+#pragma unroll
+    for (int u = 0; u < COPIES; ++u) {
+      const int slot = u * 256 + (int)threadIdx.x, r0 = slot / (DH / 8);
+      const uint32_t chunk = ((slot % (DH / 8)) ^ row_swizzle<DH>(r0)) * 16;
+      const uint32_t r = (uint32_t)min(r0, nq - 1 - q0);
+      const uint32_t at = lds_addr(smem + buf * 2 * TILE_BYTES + u * 4096 + wave * 1024);
+      dma16_at(qb, r * (uint32_t)a.Q.row + chunk, at);
+      dma16_at(yb, r * (uint32_t)a.dY.row + chunk, at + TILE_BYTES);
+    }
+    if (wave == 0) {
+      const int64_t at = (int64_t)head * a.Tq + sq.first + q0 + min(i, nq - 1 - q0);
+      dma4(h ? a.D + at : a.lse + at, lds_addr(stat[buf]));
+    }
+  };
+  f32x16 ok[DT], ov[DT];
+#pragma unroll
+  for (int d = 0; d < DT; ++d)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) ok[d][r] = ov[d][r] = 0.f;
+  bool bad = false;
+
+  if (steps > 0) fetch(0, begin, 0);
+  int g = 0, q0 = begin;
+  for (int t = 0; t < steps; ++t) {
+    int gn = g, qn = q0 + kTileQueries;
+    if (qn >= nq) { qn = begin; ++gn; }
+    wait_vmcnt<0>();
+    __syncthreads();
+    if (t + 1 < steps) fetch(gn, qn, (t + 1) & 1);
+    const int here = q0;
+    g = gn;
+    q0 = qn;
+    // (no query of the tile sees any of the wavefront's keys)
+    if (a.causal && here + kTileQueries - 1 < j0 - ahead) continue;
+    const char* qt = smem + (t & 1) * 2 * TILE_BYTES;
+    const char* yt = qt + TILE_BYTES;
+    const float* st = stat[t & 1];
+    const bool masked = here + kTileQueries > nq || (a.causal && here < j0 + 31 - ahead);
+    if (masked) {
+#pragma unroll
+      for (int u = 0; u < 2 * TILE_BYTES / 1024; ++u) bad |= any_not_finite(*reinterpret_cast<const u32x4*>(qt + u * 1024 + lane * 16));
+    }
+    f32x16 s, dp;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[r] = dp[r] = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(row_frag<DH>(qt, i, ks, h), kf[ks], s, 0, 0, 0);
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(row_frag<DH>(yt, i, ks, h), vf[ks], dp, 0, 0, 0);
+    float p[16], ds[16];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const f32x4 lse = *reinterpret_cast<const f32x4*>(st + 8 * q + 4 * h), D = *reinterpret_cast<const f32x4*>(st + 32 + 8 * q + 4 * h);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int r = 4 * q + e;
+        p[r] = __builtin_amdgcn_exp2f(fmaf(s[r], a.c, -row_offset(lse[e])));
+        ds[r] = p[r] * (dp[r] - D[e]);
+      }
+    }
+    if (masked) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int q = here + 8 * (r >> 2) + 4 * h + (r & 3);
+        const bool sees = q >= first && q < nq;
+        p[r] = sees ? p[r] : 0.f;
+        ds[r] = sees ? ds[r] : 0.f;
+      }
+    }
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      const bf16x8 pf = pack8(p + 8 * half), sf = pack8(ds + 8 * half);
+#pragma unroll
+      for (int d = 0; d < DT; ++d) ov[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(col_frag<DH>(yt, 16 * half, d, lane), pf, ov[d], 0, 0, 0);
+#pragma unroll
+      for (int d = 0; d < DT; ++d) ok[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(col_frag<DH>(qt, 16 * half, d, lane), sf, ok[d], 0, 0, 0);
+    }
+  }
+  if (__any(bad)) {
+    for (int r = 0; r < min(32, nk - j0); ++r) {
+      const int64_t at = sk.first + j0 + r;
+      slow_dkv_row<DH>(a, sq, hk, a.causal ? max(0, j0 + r - ahead) : 0, a.K.p + at * a.K.row + (int64_t)hk * a.K.head,
+                       a.V.p + at * a.V.row + (int64_t)hk * a.V.head, a.dK.p + at * a.dK.row + (int64_t)hk * a.dK.head,
+                       a.dV.p + at * a.dV.row + (int64_t)hk * a.dV.head);
+    }
+    return;
+  }
+  if (j0 + i >= nk) return;
+  char* dk = a.dK.p + (int64_t)(sk.first + mine) * a.dK.row + (int64_t)hk * a.dK.head + h * 32;
+  char* dv = a.dV.p + (int64_t)(sk.first + mine) * a.dV.row + (int64_t)hk * a.dV.head + h * 32;
+#pragma unroll
+  for (int d = 0; d < DT; ++d) {
+    float x[16], y[16];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) { x[r] = ok[d][r] * a.scale; y[r] = ov[d][r]; }
+    *reinterpret_cast<bf16x8*>(dk + d * 64) = pack8(x);
+    *reinterpret_cast<bf16x8*>(dk + d * 64 + 16) = pack8(x + 8);
+    *reinterpret_cast<bf16x8*>(dv + d * 64) = pack8(y);
+    *reinterpret_cast<bf16x8*>(dv + d * 64 + 16) = pack8(y + 8);
+  }
+}
+
+}  // namespace
+
+extern "C" size_t spt_attn_prompt_workspace_bytes(const spt_attn_shape_t* shape) {
+  if (check_attn(shape) != SPT_OK) return 0;
+  return align256((size_t)shape->H * shape->Tq * sizeof(float));
+}
+
+extern "C" int spt_attn_prompt_bwd(const spt_attn_shape_t* shape, const void* Q, const void* K, const void* V, const void* Y,
+                                   const void* dY, const float* lse, const int64_t* strides, const int32_t* cu_q, const int32_t* cu_k,
+                                   void* dQ, void* dK, void* dV, void* ws, size_t ws_bytes, void* stream) {
+  int rc = check_attn(shape);
+  if (rc != SPT_OK) return rc;
+  const spt_attn_shape_t& s = *shape;
+  BwdArgs a;
+  const struct { AttnRows* r; const void* p; bool query, out; } rows[8] = {
+      {&a.Q, Q, true, false}, {&a.K, K, false, false}, {&a.V, V, false, false}, {&a.Y, Y, true, false}, {&a.dY, dY, true, false},
+      {&a.dQ, dQ, true, true}, {&a.dK, dK, false, true}, {&a.dV, dV, false, true}};
+  for (int n = 0; n < 8; ++n) {
+    rc = attn_rows(rows[n].r, rows[n].p, strides ? strides + 2 * n : nullptr, rows[n].query ? s.Tq : s.Tk, rows[n].query ? s.H : s.Hk, s.dh,
+                   rows[n].out);
+    if (rc != SPT_OK) return rc;
+  }
+  if (!aligned_to(cu_q, 4) || !aligned_to(cu_k, 4) || !aligned_to(lse, 4) || !aligned_to(ws, 256)) return SPT_ERR_ARG;
+  if (ws_bytes < spt_attn_prompt_workspace_bytes(shape)) return SPT_ERR_WORKSPACE;
+  a.cu_q = cu_q; a.cu_k = cu_k; a.lse = lse; a.D = static_cast<float*>(ws);
+  a.B = s.B; a.Tq = s.Tq; a.Tk = s.Tk; a.Hk = s.Hk; a.G = s.H / s.Hk;
+  a.hshift = attn_heads_shift(a.G);
+  a.causal = s.causal;
+  a.scale = s.scale;
+  a.c = s.scale * kLog2e;
+  const hipStream_t st = static_cast<hipStream_t>(stream);
+  {
+    ScopedKernelTimer timer(kSlotAttnBwdQ, st);
+    a.tiles = (int)(((int64_t)s.Tq >> (7 - a.hshift)) + s.B);
+    a.units = a.tiles * s.Hk * (a.G >> a.hshift);
+    if (s.dh == 128) hipLaunchKernelGGL(prompt_bwd_q_kernel<128>, dim3(a.units), dim3(256), 0, st, a);
+    else hipLaunchKernelGGL(prompt_bwd_q_kernel<64>, dim3(a.units), dim3(256), 0, st, a);
+    if (hipGetLastError() != hipSuccess) return SPT_ERR_HIP;
+  }
+  ScopedKernelTimer timer(kSlotAttnBwdKV, st);
+  a.tiles = s.Tk / kOwnKeys + s.B;
+  a.units = a.tiles * s.Hk;
+  if (s.dh == 128) hipLaunchKernelGGL(prompt_bwd_kv_kernel<128>, dim3(a.units), dim3(256), 0, st, a);
+  else hipLaunchKernelGGL(prompt_bwd_kv_kernel<64>, dim3(a.units), dim3(256), 0, st, a);
+  return hipGetLastError() == hipSuccess ? SPT_OK : SPT_ERR_HIP;
+}

@@ -19,7 +19,8 @@ const char* kNames[kNumSlots] = {
     "router_logits", "topk", "bucket_hist", "bucket_scan", "bucket_scatter", "plan",
     "up_gemm", "down_gemm", "combine_y", "dh_gemm", "dw2_gemm", "dw1_gemm", "dx_gemm", "combine_dx", "lora_small", "lora_grad", "router_balance",
     "mha_pq_assign", "mha_topl", "mha_attn_fwd", "mha_attn_bwd_q", "mha_transpose", "mha_attn_bwd_kv",
-    "dx_dw_gemm"};
+    "dx_dw_gemm",
+    "attn_prompt_fwd", "attn_prompt_bwd_q", "attn_prompt_bwd_kv", "cache_write", "cache_read", "attn_decode", "attn_decode_join"};
 
 hipEvent_t take_event() {
   if (!g_pool.empty()) { hipEvent_t e = g_pool.back(); g_pool.pop_back(); return e; }

@@ -11,6 +11,7 @@ enum KernelSlot {
   kSlotCombineDX, kSlotLoraSmall, kSlotLoraGrad, kSlotBalance,
   kSlotMhaPq, kSlotMhaTopl, kSlotMhaFwd, kSlotMhaBwdQ, kSlotMhaTranspose, kSlotMhaBwdKV,
   kSlotDXDW,   // dX and both weight gradients in one launch, and the sum of the gradients' pieces
+  kSlotAttnFwd, kSlotAttnBwdQ, kSlotAttnBwdKV, kSlotCacheWrite, kSlotCacheRead, kSlotAttnDecode, kSlotAttnDecodeJoin,
   kNumSlots
 };
 
