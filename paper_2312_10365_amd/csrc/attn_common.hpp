@@ -108,24 +108,42 @@ __device__ __forceinline__ void dma4_at(const void* base, uint32_t off, uint32_t
 }
 __device__ __forceinline__ uint32_t lds_addr(const void* p) { return __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)p); }
 
-// Fragment reads of a row tile.  row_frag: 8 dims (16 ks + 8 h ..) of row `row`, the operand whose K is the head dimension;
-// `base` = the lane's row_frag_base.  col_frag: 4 + 4 rows of one dim, the operand whose K are the rows.
-template <int DH>
-__device__ __forceinline__ bf16x8 row_frag(const char* tile, int row, int ks, int h) {
-  return *reinterpret_cast<const bf16x8*>(tile + row * (DH * 2) + (((uint32_t)(2 * ks + h) ^ row_swizzle<DH>(row)) * 16));
+// LDS by its 32-bit address.
+template <class T>
+__device__ __forceinline__ T lds_read(uint32_t at) {
+  return *reinterpret_cast<const __attribute__((address_space(3))) T*>((uintptr_t)at);
 }
-// Transposed operand of 32 dims (dt) x 16 rows (row0 ..): MFMA row i is dim 32 dt + rho32(i), so that a lane's 16 results are
-// adjacent dims; K slot (h, e) is row row0 + 8 (e / 4) + 4 h + e % 4, the order in which a lane holds the results
-// of a product whose rows are these.
-template <int DH>
-__device__ __forceinline__ bf16x8 col_frag(const char* tile, int row0, int dt, int lane) {
-  const int g = lane >> 4, sl = lane & 15, a4 = sl & 3;
-  const int row = row0 + 4 * (g >> 1) + (sl >> 2);
-  const uint32_t chunk = dt * 4 + 2 * (a4 & 1) + (g & 1);
-  const char* lo = tile + row * (DH * 2) + (chunk ^ row_swizzle<DH>(row)) * 16 + (a4 >> 1) * 8;
-  const char* hi = tile + (row + 8) * (DH * 2) + (chunk ^ row_swizzle<DH>(row + 8)) * 16 + (a4 >> 1) * 8;
-  return tr_read_frag(lo, hi);
+__device__ __forceinline__ bf16x8 lds_tr_read(uint32_t lo, uint32_t hi) {
+  struct { v4s a, b; } t;
+  t.a = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lds_v4s_ptr>((uintptr_t)lo));
+  t.b = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lds_v4s_ptr>((uintptr_t)hi));
+  return __builtin_bit_cast(bf16x8, t);
 }
+
+// Operands out of a row tile (256-byte aligned).
+// rows(): 8 dims (16 ks + 8 h ..) of row 32 n + lane % 32, the operand whose K is the head dimension.
+// columns(): 32 dims (32 d ..) x 16 rows (16 n ..), transposed, the operand whose K are the rows.  MFMA row i is dim 32 d + rho32(i), so
+// that a lane's 16 results are adjacent dims; K slot (h, e) is row 16 n + 8 (e / 4) + 4 h + e % 4, the order in which a
+// lane holds the results of a product whose rows are these.
+// Everything but two words per lane is an exclusive-or with a constant or an offset in the instruction: `fresh` keeps the
+// compiler from computing all addresses in front of a loop, for which there are no registers.
+template <int DH>
+struct TileReader {
+  uint32_t row, col;   // offsets in a tile
+  __device__ __forceinline__ explicit TileReader(int lane) {
+    const int i = lane & 31, h = lane >> 5, g = lane >> 4, sl = lane & 15, a4 = sl & 3, r = 4 * (g >> 1) + (sl >> 2);
+    row = i * (DH * 2) + ((uint32_t)h ^ row_swizzle<DH>(i)) * 16;
+    col = r * (DH * 2) + ((uint32_t)(2 * (a4 & 1) + (g & 1)) ^ row_swizzle<DH>(r)) * 16 + (a4 >> 1) * 8;
+  }
+  __device__ __forceinline__ void fresh() { asm volatile("" : "+v"(row), "+v"(col)); }
+  __device__ __forceinline__ bf16x8 rows(uint32_t tile, int n, int ks) const {
+    return lds_read<bf16x8>((tile + row ^ (uint32_t)(ks * 32)) + n * (32 * DH * 2));
+  }
+  __device__ __forceinline__ bf16x8 columns(uint32_t tile, int n, int d) const {
+    const uint32_t lo = tile + col ^ (uint32_t)(d * 64);
+    return lds_tr_read(lo + n * (16 * DH * 2), (lo ^ 16u) + (n * 16 + 8) * (DH * 2));   // (rows 8 on: bit 3 of the row is in the swizzle)
+  }
+};
 
 __device__ __forceinline__ float other_half(float x) {   // the value of the lane 32 away
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);

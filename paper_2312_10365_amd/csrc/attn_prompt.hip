@@ -103,6 +103,8 @@ __global__ __launch_bounds__(256, 2) void prompt_fwd_kernel(const FwdArgs a) {
       dma16_at(vb, r * (uint32_t)a.V.row + chunk, at + TILE_BYTES);
     }
   };
+  TileReader<DH> lds(lane);
+  const uint32_t tiles = lds_addr(smem);
   f32x16 o[DT];
 #pragma unroll
   for (int d = 0; d < DT; ++d)
@@ -118,8 +120,8 @@ __global__ __launch_bounds__(256, 2) void prompt_fwd_kernel(const FwdArgs a) {
     if (t + 1 < ntile) fetch(t + 1, (t + 1) & 1);
     const int j0 = t * kTileKeys;
     if (j0 >= wave_kend) continue;
-    const char* kt_ = smem + (t & 1) * 2 * TILE_BYTES;
-    const char* vt_ = kt_ + TILE_BYTES;
+    const uint32_t kt_ = tiles + (t & 1) * 2 * TILE_BYTES, vt_ = kt_ + TILE_BYTES;
+    lds.fresh();
     f32x16 s[2];
 #pragma unroll
     for (int kt = 0; kt < 2; ++kt) {
@@ -127,7 +129,7 @@ __global__ __launch_bounds__(256, 2) void prompt_fwd_kernel(const FwdArgs a) {
       for (int r = 0; r < 16; ++r) s[kt][r] = 0.f;
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks)
-        s[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(row_frag<DH>(kt_, 32 * kt + i, ks, h), qf[ks], s[kt], 0, 0, 0);
+        s[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lds.rows(kt_, kt, ks), qf[ks], s[kt], 0, 0, 0);
     }
     if (j0 + kTileKeys > wave_full) {
       const int left = seen - j0 - 4 * h;
@@ -137,7 +139,7 @@ __global__ __launch_bounds__(256, 2) void prompt_fwd_kernel(const FwdArgs a) {
         for (int r = 0; r < 16; ++r) s[kt][r] = 32 * kt + 8 * (r >> 2) + (r & 3) < left ? s[kt][r] : -INFINITY;
       // rows of V that some query must not see: 0 times an infinity is NaN
 #pragma unroll
-      for (int u = 0; u < TILE_BYTES / 1024; ++u) bad |= any_not_finite(*reinterpret_cast<const u32x4*>(vt_ + u * 1024 + lane * 16));
+      for (int u = 0; u < TILE_BYTES / 1024; ++u) bad |= any_not_finite(lds_read<u32x4>(vt_ + u * 1024 + lane * 16));
     }
     float top = s[0][0];
 #pragma unroll
@@ -173,7 +175,7 @@ __global__ __launch_bounds__(256, 2) void prompt_fwd_kernel(const FwdArgs a) {
       for (int half = 0; half < 2; ++half)
 #pragma unroll
         for (int d = 0; d < DT; ++d)
-          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(col_frag<DH>(vt_, 32 * kt + 16 * half, d, lane), pf[kt][half], o[d], 0, 0, 0);
+          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lds.columns(vt_, 2 * kt + half, d), pf[kt][half], o[d], 0, 0, 0);
   }
 
   float* lse = a.lse ? a.lse + (int64_t)head * a.Tq + sq.first : nullptr;

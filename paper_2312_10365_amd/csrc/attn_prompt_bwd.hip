@@ -17,13 +17,14 @@ using namespace spt;
 
 namespace {
 
-constexpr int kTileKeys = 64, kTileQueries = 32, kOwnKeys = 128;
+constexpr int kTile = 32, kOwnKeys = 128;   // rows of a tile that passes through LDS; keys of a workgroup
+constexpr int kRing = 2;                    // tiles in LDS: one in use, one being filled
 
 struct BwdArgs {
   AttnRows Q, K, V, Y, dY, dQ, dK, dV;
   const int32_t *cu_q, *cu_k;
   const float* lse;
-  float* D;                       // [H][Tq]
+  float *off, *neg_d;             // [H][Tq]: row_offset(lse), -D
   int B, Tq, Tk, Hk, G, hshift;
   int tiles, units;               // of the launch
   int causal;
@@ -33,11 +34,30 @@ struct BwdArgs {
 // exp2 argument's subtrahend of a row: rows without a key have lse = -inf and p = 0
 __device__ __forceinline__ float row_offset(float lse) { return lse == -INFINITY ? INFINITY : lse * kLog2e; }
 
+// P and dS of 32 x 32 pairs as operands of the second products: a lane's results 8 half .. 8 half + 7.
+struct Weights { u32x4 p[2], ds[2]; };
+
 // p and dS of one pair, from its rows in memory.
 struct PairGrad { float p, ds; };
 __device__ __forceinline__ PairGrad pair_grad(const char* q, const char* k, const char* dy, const char* v, int dh, float c, float off, float D) {
   const float p = __builtin_amdgcn_exp2f(fmaf(row_dot(q, k, dh), c, -off));
   return {p, p * (row_dot(dy, v, dh) - D)};
+}
+
+// Rows q0 .. q0 + 31 of two tensors of n rows into a pair of tiles (rows past the end: the last one again).
+template <int DH>
+__device__ __forceinline__ void fetch_pair(const char* x, int64_t xrow, const char* y, int64_t yrow, int q0, int n, const char* tiles, int wave) {
+  constexpr int COPIES = kTile * (DH / 8) / 256;
+  const char* xb = x + q0 * xrow;
+  const char* yb = y + q0 * yrow;
+#pragma unroll
+  for (int u = 0; u < COPIES; ++u) {
+    const int slot = u * 256 + (int)threadIdx.x, r0 = slot / (DH / 8);
+    const uint32_t chunk = ((slot % (DH / 8)) ^ row_swizzle<DH>(r0)) * 16, r = (uint32_t)min(r0, n - 1 - q0);
+    const uint32_t at = lds_addr(tiles + u * 4096 + wave * 1024);
+    dma16_at(xb, r * (uint32_t)xrow + chunk, at);
+    dma16_at(yb, r * (uint32_t)yrow + chunk, at + kTile * DH * 2);
+  }
 }
 
 template <int DH>
@@ -59,9 +79,11 @@ __device__ __forceinline__ void slow_dq_row(const BwdArgs& a, const char* q, con
 }
 
 template <int DH>
-__global__ __launch_bounds__(256, DH == 128 ? 1 : 2) void prompt_bwd_q_kernel(const BwdArgs a) {
-  constexpr int KS = DH / 16, DT = DH / 32, TILE_BYTES = kTileKeys * DH * 2;
-  __shared__ __align__(256) char smem[4 * TILE_BYTES];
+__global__ __launch_bounds__(256, 2) void prompt_bwd_q_kernel(const BwdArgs a) {
+  constexpr int KS = DH / 16, DT = DH / 32, TILE_BYTES = kTile * DH * 2;
+  // 128-wide heads: dY of the wavefront's rows stays in LDS, or two wavefronts would not fit into a SIMD's registers
+  constexpr bool OWN = DH == 128;
+  __shared__ __align__(256) char smem[(kRing * 2 + (OWN ? 4 : 0)) * TILE_BYTES];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 31, h = lane >> 5;
   const int hsets = a.G >> a.hshift, unit = xcd_contiguous(blockIdx.x, a.units);
   const int hk = unit / (hsets * a.tiles), rest = unit - hk * (hsets * a.tiles);
@@ -80,41 +102,33 @@ __global__ __launch_bounds__(256, DH == 128 ? 1 : 2) void prompt_bwd_q_kernel(co
   const int wave_full = i0 >= nq ? 0 : a.causal ? min(nk, i0 + ahead + 1) : nk;
   const int mine = min(i0 + i, nq - 1);
   const int seen = a.causal ? min(nk, mine + ahead + 1) : nk;
-  const int ntile = kend > 0 ? (kend + kTileKeys - 1) / kTileKeys : 0;
+  const int ntile = kend > 0 ? (kend + kTile - 1) / kTile : 0;
+
+  const char* kbase = a.K.p + (int64_t)sk.first * a.K.row + (int64_t)hk * a.K.head;
+  const char* vbase = a.V.p + (int64_t)sk.first * a.V.row + (int64_t)hk * a.V.head;
+  auto fetch = [&](int t) { fetch_pair<DH>(kbase, a.K.row, vbase, a.V.row, t * kTile, nk, smem + t % kRing * 2 * TILE_BYTES, wave); };
+  if (ntile > 0) fetch(0);
 
   const int64_t row = sq.first + mine;
   const char* qrow = a.Q.p + row * a.Q.row + (int64_t)head * a.Q.head;
   const char* yrow = a.Y.p + row * a.Y.row + (int64_t)head * a.Y.head;
   const char* dyrow = a.dY.p + row * a.dY.row + (int64_t)head * a.dY.head;
-  bf16x8 qf[KS], dyf[KS];
+  bf16x8 qf[KS], dyf[OWN ? 1 : KS];
+  TileReader<DH> lds(lane);
+  const uint32_t tiles = lds_addr(smem), own = tiles + (kRing * 2 + wave) * TILE_BYTES;
   float D = 0.f;
 #pragma unroll
   for (int s = 0; s < KS; ++s) {
     qf[s] = *reinterpret_cast<const bf16x8*>(qrow + s * 32 + h * 16);
     const u32x4 dy = *reinterpret_cast<const u32x4*>(dyrow + s * 32 + h * 16), y = *reinterpret_cast<const u32x4*>(yrow + s * 32 + h * 16);
-    dyf[s] = as_bf16x8(dy);
+    if (OWN) *reinterpret_cast<u32x4*>(smem + (kRing * 2 + wave) * TILE_BYTES + (lds.row ^ (uint32_t)(s * 32))) = dy;
+    else dyf[s] = as_bf16x8(dy);
 #pragma unroll
     for (int e = 0; e < 4; ++e) D = fmaf(hi_bf16(dy[e]), hi_bf16(y[e]), fmaf(lo_bf16(dy[e]), lo_bf16(y[e]), D));
   }
   D += other_half(D);
   const float off = row_offset(a.lse[(int64_t)head * a.Tq + row]);
-  const char* kbase = a.K.p + (int64_t)sk.first * a.K.row + (int64_t)hk * a.K.head;
-  const char* vbase = a.V.p + (int64_t)sk.first * a.V.row + (int64_t)hk * a.V.head;
-  constexpr int COPIES = kTileKeys * (DH / 8) / 256;
-  auto fetch = [&](int t, int buf) {
-    const int j0 = t * kTileKeys;
-    const char* kb = kbase + (int64_t)j0 * a.K.row;
-    const char* vb = vbase + (int64_t)j0 * a.V.row;
-#pragma unroll
-    for (int u = 0; u < COPIES; ++u) {
-      const int slot = u * 256 + (int)threadIdx.x, r0 = slot / (DH / 8);
-      const uint32_t chunk = ((slot % (DH / 8)) ^ row_swizzle<DH>(r0)) * 16;
-      const uint32_t r = (uint32_t)min(r0, nk - 1 - j0);
-      const uint32_t at = lds_addr(smem + buf * 2 * TILE_BYTES + u * 4096 + wave * 1024);
-      dma16_at(kb, r * (uint32_t)a.K.row + chunk, at);
-      dma16_at(vb, r * (uint32_t)a.V.row + chunk, at + TILE_BYTES);
-    }
-  };
+
   f32x16 o[DT], mean[DT];                                // sums of dS k and of p k
 #pragma unroll
   for (int d = 0; d < DT; ++d)
@@ -123,74 +137,92 @@ __global__ __launch_bounds__(256, DH == 128 ? 1 : 2) void prompt_bwd_q_kernel(co
   float left_over = 0.f;                                 // sum of dS: what D lacks
   bool bad = false;
 
-  if (ntile > 0) fetch(0, 0);
-  for (int t = 0; t < ntile; ++t) {
-    wait_vmcnt<0>();
-    __syncthreads();
-    if (t + 1 < ntile) fetch(t + 1, (t + 1) & 1);
-    const int j0 = t * kTileKeys;
-    if (j0 >= wave_kend) continue;
-    const char* kt_ = smem + (t & 1) * 2 * TILE_BYTES;
-    const char* vt_ = kt_ + TILE_BYTES;
-    const bool masked = j0 + kTileKeys > wave_full;
-    if (masked) {
+  auto first_products = [&](int t, f32x16& s, f32x16& dp) {
+    const uint32_t kt = tiles + (t % kRing) * 2 * TILE_BYTES;
+    lds.fresh();
 #pragma unroll
-      for (int u = 0; u < TILE_BYTES / 1024; ++u) bad |= any_not_finite(*reinterpret_cast<const u32x4*>(kt_ + u * 1024 + lane * 16));
+    for (int r = 0; r < 16; ++r) s[r] = dp[r] = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lds.rows(kt, 0, ks), qf[ks], s, 0, 0, 0);
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+      dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lds.rows(kt + TILE_BYTES, 0, ks), OWN ? lds.rows(own, 0, ks) : dyf[OWN ? 0 : ks], dp, 0, 0, 0);
+  };
+  auto weights = [&](int t, f32x16& s, f32x16& dp, bool masked) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      s[r] = fmaf(s[r], a.c, -off);
+      dp[r] -= D;
     }
-#pragma unroll
-    for (int kt = 0; kt < 2; ++kt) {
-      f32x16 s, dp;
-#pragma unroll
-      for (int r = 0; r < 16; ++r) s[r] = dp[r] = 0.f;
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks)
-        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(row_frag<DH>(kt_, 32 * kt + i, ks, h), qf[ks], s, 0, 0, 0);
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks)
-        dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(row_frag<DH>(vt_, 32 * kt + i, ks, h), dyf[ks], dp, 0, 0, 0);
-      float p[16], ds[16];
+    if (masked) {
+      const int left = seen - t * kTile - 4 * h;
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        p[r] = __builtin_amdgcn_exp2f(fmaf(s[r], a.c, -off));
-        ds[r] = p[r] * (dp[r] - D);
-      }
-      if (masked) {
-        const int left = seen - j0 - 32 * kt - 4 * h;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const bool sees = 8 * (r >> 2) + (r & 3) < left;
-          p[r] = sees ? p[r] : 0.f;
-          ds[r] = sees ? ds[r] : 0.f;
-        }
-      }
-#pragma unroll
-      for (int r = 0; r < 16; ++r) left_over += ds[r];
-#pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        const bf16x8 pf = pack8(p + 8 * half), sf = pack8(ds + 8 * half);
-#pragma unroll
-        for (int d = 0; d < DT; ++d) {
-          const bf16x8 f = col_frag<DH>(kt_, 32 * kt + 16 * half, d, lane);
-          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, sf, o[d], 0, 0, 0);
-          mean[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, pf, mean[d], 0, 0, 0);
-        }
+        const bool sees = 8 * (r >> 2) + (r & 3) < left;
+        s[r] = sees ? s[r] : -INFINITY;
+        dp[r] = sees ? dp[r] : 0.f;
       }
     }
+    Weights w;
+#pragma unroll
+    for (int r = 0; r < 16; r += 2) {
+      const float p0 = __builtin_amdgcn_exp2f(s[r]), p1 = __builtin_amdgcn_exp2f(s[r + 1]), d0 = p0 * dp[r], d1 = p1 * dp[r + 1];
+      left_over += d0 + d1;
+      w.p[r >> 3][(r & 7) >> 1] = pack_bf16x2(p0, p1);
+      w.ds[r >> 3][(r & 7) >> 1] = pack_bf16x2(d0, d1);
+    }
+    return w;
+  };
+  auto second_products = [&](int t, const Weights& w) {
+    const uint32_t kt = tiles + (t % kRing) * 2 * TILE_BYTES;
+    lds.fresh();
+#pragma unroll
+    for (int half = 0; half < 2; ++half)
+#pragma unroll
+      for (int d = 0; d < DT; ++d) {
+        const bf16x8 f = lds.columns(kt, half, d);
+        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, as_bf16x8(w.ds[half]), o[d], 0, 0, 0);
+        mean[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, as_bf16x8(w.p[half]), mean[d], 0, 0, 0);
+      }
+  };
+  auto turn = [&](int t) {                               // tile t is there; asks for the next
+    wait_vmcnt<0>();
+    __syncthreads();
+    if (t + 1 < ntile) fetch(t + 1);
+  };
+  for (int t = 0; t < ntile; ++t) {
+    turn(t);
+    const int j0 = t * kTile;
+    if (j0 >= wave_kend) continue;
+    const bool masked = j0 + kTile > wave_full;
+    if (masked) {
+#pragma unroll
+      for (int u = 0; u < TILE_BYTES / 1024; ++u) bad |= any_not_finite(lds_read<u32x4>(tiles + (t % kRing) * 2 * TILE_BYTES + u * 1024 + lane * 16));
+    }
+    f32x16 s, dp;
+    first_products(t, s, dp);
+    second_products(t, weights(t, s, dp, masked));
   }
-  float* Dout = a.D + (int64_t)head * a.Tq;
+  left_over += other_half(left_over);
+  const int64_t stat = (int64_t)head * a.Tq;
   if (__any(bad)) {
     for (int r = 0; r < min(32, nq - i0); ++r) {
       const int64_t at = sq.first + i0 + r;
       const float Dr = __shfl(D, r), offr = __shfl(off, r);
-      if (lane == 0) Dout[at] = Dr;
+      if (lane == 0) {
+        a.off[stat + at] = offr;
+        a.neg_d[stat + at] = -Dr;
+      }
       slow_dq_row<DH>(a, a.Q.p + at * a.Q.row + (int64_t)head * a.Q.head, a.dY.p + at * a.dY.row + (int64_t)head * a.dY.head, kbase, vbase,
                       a.causal ? min(nk, i0 + r + ahead + 1) : nk, offr, Dr, a.dQ.p + at * a.dQ.row + (int64_t)head * a.dQ.head);
     }
     return;
   }
   if (i0 + i >= nq) return;
-  left_over += other_half(left_over);
-  if (h == 0) Dout[row] = D + left_over;
+  if (h == 0) {
+    a.off[stat + row] = off;
+    a.neg_d[stat + row] = -(D + left_over);
+  }
   char* dq = a.dQ.p + row * a.dQ.row + (int64_t)head * a.dQ.head + h * 32;
 #pragma unroll
   for (int d = 0; d < DT; ++d) {
@@ -215,7 +247,7 @@ __device__ __forceinline__ void slow_dkv_row(const BwdArgs& a, const SeqRows& sq
     for (int i0 = first; i0 < sq.n; i0 += 64) {
       const int i = i0 + lane;
       PairGrad x = {0.f, 0.f};
-      if (i < sq.n) x = pair_grad(q + i * a.Q.row, k, dy + i * a.dY.row, v, DH, a.c, row_offset(a.lse[stat + i]), a.D[stat + i]);
+      if (i < sq.n) x = pair_grad(q + i * a.Q.row, k, dy + i * a.dY.row, v, DH, a.c, a.off[stat + i], -a.neg_d[stat + i]);
       for (int e = 0; e < min(64, sq.n - i0); ++e) {
         const float p = __shfl(x.p, e), ds = __shfl(x.ds, e);
 #pragma unroll
@@ -234,10 +266,11 @@ __device__ __forceinline__ void slow_dkv_row(const BwdArgs& a, const SeqRows& sq
 }
 
 template <int DH>
-__global__ __launch_bounds__(256, 1) void prompt_bwd_kv_kernel(const BwdArgs a) {
-  constexpr int KS = DH / 16, DT = DH / 32, TILE_BYTES = kTileQueries * DH * 2;
-  __shared__ __align__(256) char smem[4 * TILE_BYTES];    // Q, dY, twice
-  __shared__ __align__(256) float stat[2][64];            // lse, D of a tile's rows
+__global__ __launch_bounds__(256, 2) void prompt_bwd_kv_kernel(const BwdArgs a) {
+  constexpr int KS = DH / 16, DT = DH / 32, TILE_BYTES = kTile * DH * 2;
+  constexpr bool OWN = DH == 128;                                // V of the wavefront's keys stays in LDS, as above
+  __shared__ __align__(256) char smem[(kRing * 2 + (OWN ? 4 : 0)) * TILE_BYTES];   // Q, dY
+  __shared__ __align__(256) float stat[kRing][64];               // a tile's rows' offsets and -D
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 31, h = lane >> 5;
   const int unit = xcd_contiguous(blockIdx.x, a.units), hk = unit / a.tiles;
   int b, tile;
@@ -247,36 +280,43 @@ __global__ __launch_bounds__(256, 1) void prompt_bwd_kv_kernel(const BwdArgs a) 
   const int nq = sq.n, nk = sk.n, ahead = nk - nq;
   const int j0 = tile * kOwnKeys + wave * 32, mine = min(j0 + i, nk - 1);
   const int first = a.causal ? max(0, mine - ahead) : 0;                 // the first query that sees the lane's key
-  const int begin = a.causal ? max(0, tile * kOwnKeys - ahead) & ~(kTileQueries - 1) : 0;
-  const int nt = begin < nq ? (nq - begin + kTileQueries - 1) / kTileQueries : 0, steps = nt * a.G;
+  const int begin = a.causal ? max(0, tile * kOwnKeys - ahead) & ~(kTile - 1) : 0;
+  // Tiles of a head from `begin` on: in front of `full` some query does not see some key of the workgroup, the last one may be
+  // short, the others need no mask.  Steps: the masked tiles of all heads, then the others.
+  const int full = a.causal ? max(begin, (tile * kOwnKeys + kOwnKeys - 1 - ahead + kTile - 1) & ~(kTile - 1)) : 0;
+  const int tail = nq & ~(kTile - 1), front = max(0, min(full, nq) - begin + kTile - 1) / kTile;
+  const int head_masked = front + (tail < nq && tail >= full), head_full = max(0, tail - full) / kTile;
+  const int masked_steps = head_masked * a.G, steps = masked_steps + head_full * a.G;
+  const int wave_begin = a.causal ? j0 - ahead - (kTile - 1) : 0;        // tiles from here on have a query that sees a key of the wavefront
+
+  struct Place { int g, x; };                                            // a step's head, and its tile among the masked or the others
+  auto first_query = [&](int t, const Place& p) { return t >= masked_steps ? full + p.x * kTile : p.x < front ? begin + p.x * kTile : tail; };
+  auto after = [&](int t, const Place& p) {
+    if (p.x + 1 < (t < masked_steps ? head_masked : head_full)) return Place{p.g, p.x + 1};
+    return t + 1 == masked_steps ? Place{0, 0} : Place{p.g + 1, 0};
+  };
+  auto fetch = [&](int t, const Place& p) {
+    const int head = hk * a.G + p.g, q0 = first_query(t, p), buf = t % kRing;
+    fetch_pair<DH>(a.Q.p + (int64_t)sq.first * a.Q.row + (int64_t)head * a.Q.head, a.Q.row,
+                   a.dY.p + (int64_t)sq.first * a.dY.row + (int64_t)head * a.dY.head, a.dY.row, q0, nq, smem + buf * 2 * TILE_BYTES, wave);
+    const int64_t at = (int64_t)head * a.Tq + sq.first + q0 + min(i, nq - 1 - q0);
+    if (wave == 0) dma4(h ? a.neg_d + at : a.off + at, lds_addr(stat[buf]));
+  };
+  Place coming = {0, 0};                                                 // of the last step asked for
+  if (steps > 0) fetch(0, coming);
 
   const char* krow = a.K.p + (int64_t)(sk.first + mine) * a.K.row + (int64_t)hk * a.K.head;
   const char* vrow = a.V.p + (int64_t)(sk.first + mine) * a.V.row + (int64_t)hk * a.V.head;
-  bf16x8 kf[KS], vf[KS];
+  bf16x8 kf[KS], vf[OWN ? 1 : KS];
+  TileReader<DH> lds(lane);
+  const uint32_t tiles = lds_addr(smem), own = tiles + (kRing * 2 + wave) * TILE_BYTES;
 #pragma unroll
   for (int s = 0; s < KS; ++s) {
     kf[s] = *reinterpret_cast<const bf16x8*>(krow + s * 32 + h * 16);
-    vf[s] = *reinterpret_cast<const bf16x8*>(vrow + s * 32 + h * 16);
+    const bf16x8 v = *reinterpret_cast<const bf16x8*>(vrow + s * 32 + h * 16);
+    if (OWN) *reinterpret_cast<bf16x8*>(smem + (kRing * 2 + wave) * TILE_BYTES + (lds.row ^ (uint32_t)(s * 32))) = v;
+    else vf[s] = v;
   }
-  constexpr int COPIES = kTileQueries * (DH / 8) / 256;
-  auto fetch = [&](int g, int q0, int buf) {
-    const int head = hk * a.G + g;
-    const char* qb = a.Q.p + (int64_t)(sq.first + q0) * a.Q.row + (int64_t)head * a.Q.head;
-    const char* yb = a.dY.p + (int64_t)(sq.first + q0) * a.dY.row + (int64_t)head * a.dY.head;
-#pragma unroll
-    for (int u = 0; u < COPIES; ++u) {
-      const int slot = u * 256 + (int)threadIdx.x, r0 = slot / (DH / 8);
-      const uint32_t chunk = ((slot % (DH / 8)) ^ row_swizzle<DH>(r0)) * 16;
-      const uint32_t r = (uint32_t)min(r0, nq - 1 - q0);
-      const uint32_t at = lds_addr(smem + buf * 2 * TILE_BYTES + u * 4096 + wave * 1024);
-      dma16_at(qb, r * (uint32_t)a.Q.row + chunk, at);
-      dma16_at(yb, r * (uint32_t)a.dY.row + chunk, at + TILE_BYTES);
-    }
-    if (wave == 0) {
-      const int64_t at = (int64_t)head * a.Tq + sq.first + q0 + min(i, nq - 1 - q0);
-      dma4(h ? a.D + at : a.lse + at, lds_addr(stat[buf]));
-    }
-  };
   f32x16 ok[DT], ov[DT];
 #pragma unroll
   for (int d = 0; d < DT; ++d)
@@ -284,62 +324,85 @@ __global__ __launch_bounds__(256, 1) void prompt_bwd_kv_kernel(const BwdArgs a) 
     for (int r = 0; r < 16; ++r) ok[d][r] = ov[d][r] = 0.f;
   bool bad = false;
 
-  if (steps > 0) fetch(0, begin, 0);
-  int g = 0, q0 = begin;
-  for (int t = 0; t < steps; ++t) {
-    int gn = g, qn = q0 + kTileQueries;
-    if (qn >= nq) { qn = begin; ++gn; }
-    wait_vmcnt<0>();
-    __syncthreads();
-    if (t + 1 < steps) fetch(gn, qn, (t + 1) & 1);
-    const int here = q0;
-    g = gn;
-    q0 = qn;
-    // (no query of the tile sees any of the wavefront's keys)
-    if (a.causal && here + kTileQueries - 1 < j0 - ahead) continue;
-    const char* qt = smem + (t & 1) * 2 * TILE_BYTES;
-    const char* yt = qt + TILE_BYTES;
-    const float* st = stat[t & 1];
-    const bool masked = here + kTileQueries > nq || (a.causal && here < j0 + 31 - ahead);
-    if (masked) {
-#pragma unroll
-      for (int u = 0; u < 2 * TILE_BYTES / 1024; ++u) bad |= any_not_finite(*reinterpret_cast<const u32x4*>(qt + u * 1024 + lane * 16));
-    }
-    f32x16 s, dp;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) s[r] = dp[r] = 0.f;
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(row_frag<DH>(qt, i, ks, h), kf[ks], s, 0, 0, 0);
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(row_frag<DH>(yt, i, ks, h), vf[ks], dp, 0, 0, 0);
-    float p[16], ds[16];
+  auto first_products = [&](int t, f32x16& s, f32x16& dp) {
+    const int buf = t % kRing;
+    const uint32_t qt = tiles + buf * 2 * TILE_BYTES;
+    lds.fresh();
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-      const f32x4 lse = *reinterpret_cast<const f32x4*>(st + 8 * q + 4 * h), D = *reinterpret_cast<const f32x4*>(st + 32 + 8 * q + 4 * h);
+      const f32x4 d = *reinterpret_cast<const f32x4*>(stat[buf] + 32 + 8 * q + 4 * h);   // (dP starts from -D)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const int r = 4 * q + e;
-        p[r] = __builtin_amdgcn_exp2f(fmaf(s[r], a.c, -row_offset(lse[e])));
-        ds[r] = p[r] * (dp[r] - D[e]);
+        s[4 * q + e] = 0.f;
+        dp[4 * q + e] = d[e];
       }
+    }
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lds.rows(qt, 0, ks), kf[ks], s, 0, 0, 0);
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+      dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lds.rows(qt + TILE_BYTES, 0, ks), OWN ? lds.rows(own, 0, ks) : vf[OWN ? 0 : ks], dp, 0, 0, 0);
+  };
+  auto weights = [&](int t, int q0, f32x16& s, f32x16& dp, bool masked) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const f32x4 off = *reinterpret_cast<const f32x4*>(stat[t % kRing] + 8 * q + 4 * h);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[4 * q + e] = fmaf(s[4 * q + e], a.c, -off[e]);
     }
     if (masked) {
+      const int from = first - q0 - 4 * h, to = nq - q0 - 4 * h;
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        const int q = here + 8 * (r >> 2) + 4 * h + (r & 3);
-        const bool sees = q >= first && q < nq;
-        p[r] = sees ? p[r] : 0.f;
-        ds[r] = sees ? ds[r] : 0.f;
+        const int at = 8 * (r >> 2) + (r & 3);
+        const bool sees = at >= from && at < to;
+        s[r] = sees ? s[r] : -INFINITY;
+        dp[r] = sees ? dp[r] : 0.f;
       }
     }
+    Weights w;
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      const bf16x8 pf = pack8(p + 8 * half), sf = pack8(ds + 8 * half);
-#pragma unroll
-      for (int d = 0; d < DT; ++d) ov[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(col_frag<DH>(yt, 16 * half, d, lane), pf, ov[d], 0, 0, 0);
-#pragma unroll
-      for (int d = 0; d < DT; ++d) ok[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(col_frag<DH>(qt, 16 * half, d, lane), sf, ok[d], 0, 0, 0);
+    for (int r = 0; r < 16; r += 2) {
+      const float p0 = __builtin_amdgcn_exp2f(s[r]), p1 = __builtin_amdgcn_exp2f(s[r + 1]);
+      w.p[r >> 3][(r & 7) >> 1] = pack_bf16x2(p0, p1);
+      w.ds[r >> 3][(r & 7) >> 1] = pack_bf16x2(p0 * dp[r], p1 * dp[r + 1]);
     }
+    return w;
+  };
+  auto second_products = [&](int t, const Weights& w) {
+    const uint32_t qt = tiles + t % kRing * 2 * TILE_BYTES;
+    lds.fresh();
+#pragma unroll
+    for (int half = 0; half < 2; ++half)
+#pragma unroll
+      for (int d = 0; d < DT; ++d) {
+        ov[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lds.columns(qt + TILE_BYTES, half, d), as_bf16x8(w.p[half]), ov[d], 0, 0, 0);
+        ok[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lds.columns(qt, half, d), as_bf16x8(w.ds[half]), ok[d], 0, 0, 0);
+      }
+  };
+  auto turn = [&](int t) {                                               // step t's tile is there; asks for the next
+    wait_vmcnt<0>();
+    __syncthreads();
+    if (t + 1 < steps) {
+      coming = after(t, coming);
+      fetch(t + 1, coming);
+    }
+  };
+  Place here = {0, 0};
+  for (int t = 0; t < steps; ++t) {
+    turn(t);
+    const int q0 = first_query(t, here);
+    here = after(t, here);
+    if (q0 < wave_begin) continue;
+    const bool masked = t < masked_steps;
+    if (masked) {
+#pragma unroll
+      for (int u = 0; u < 2 * TILE_BYTES / 1024; ++u)
+        bad |= any_not_finite(lds_read<u32x4>(tiles + t % kRing * 2 * TILE_BYTES + u * 1024 + lane * 16));
+    }
+    f32x16 s, dp;
+    first_products(t, s, dp);
+    second_products(t, weights(t, q0, s, dp, masked));
   }
   if (__any(bad)) {
     for (int r = 0; r < min(32, nk - j0); ++r) {
@@ -369,7 +432,7 @@ __global__ __launch_bounds__(256, 1) void prompt_bwd_kv_kernel(const BwdArgs a) 
 
 extern "C" size_t spt_attn_prompt_workspace_bytes(const spt_attn_shape_t* shape) {
   if (check_attn(shape) != SPT_OK) return 0;
-  return align256((size_t)shape->H * shape->Tq * sizeof(float));
+  return 2 * align256((size_t)shape->H * shape->Tq * sizeof(float));
 }
 
 extern "C" int spt_attn_prompt_bwd(const spt_attn_shape_t* shape, const void* Q, const void* K, const void* V, const void* Y,
@@ -389,7 +452,8 @@ extern "C" int spt_attn_prompt_bwd(const spt_attn_shape_t* shape, const void* Q,
   }
   if (!aligned_to(cu_q, 4) || !aligned_to(cu_k, 4) || !aligned_to(lse, 4) || !aligned_to(ws, 256)) return SPT_ERR_ARG;
   if (ws_bytes < spt_attn_prompt_workspace_bytes(shape)) return SPT_ERR_WORKSPACE;
-  a.cu_q = cu_q; a.cu_k = cu_k; a.lse = lse; a.D = static_cast<float*>(ws);
+  a.cu_q = cu_q; a.cu_k = cu_k; a.lse = lse; a.off = static_cast<float*>(ws);
+  a.neg_d = a.off + align256((size_t)s.H * s.Tq * sizeof(float)) / sizeof(float);
   a.B = s.B; a.Tq = s.Tq; a.Tk = s.Tk; a.Hk = s.Hk; a.G = s.H / s.Hk;
   a.hshift = attn_heads_shift(a.G);
   a.causal = s.causal;
