@@ -28,7 +28,7 @@ extern "C" {
  * j <= i + nk - nq: the last query sees all keys, so that nq < nk is a part of a prompt behind keys
  * that are there already, and with nq > nk the first nq - nk queries see nothing. */
 typedef struct {
-  int32_t B;      /* sequences, 1 .. 65535; any of them may be empty */
+  int32_t B;      /* sequences, 1 .. 4096; any of them may be empty */
   int32_t Tq, Tk; /* rows of Q, of K and V: at least one; cu_q[B] <= Tq, cu_k[B] <= Tk */
   int32_t H, Hk;  /* query heads, key heads */
   int32_t dh;     /* 64 or 128 */

@@ -55,38 +55,94 @@ __device__ __forceinline__ SeqRows seq_rows(const int32_t* cu, int b, int T) {
   return {lo, max(0, hi - lo)};
 }
 
-// Tile t of all sequences' row tiles of `rows` rows, in order: its sequence and the tile's number in it.  All lanes of a
-// wavefront look together, 64 sequences at a time.  False: there are not so many tiles.
-__device__ __forceinline__ bool find_tile(const int32_t* cu, int B, int T, int rows_shift, int t, int& b, int& tile, SeqRows& s) {
-  const int lane = threadIdx.x & 63;
-  int before = 0;
-  for (int b0 = 0; b0 < B; b0 += 64) {
-    const int mine = b0 + lane;
-    SeqRows x = {0, 0};
-    if (mine < B) x = seq_rows(cu, mine, T);
-    int incl = (x.n + (1 << rows_shift) - 1) >> rows_shift;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int up = __shfl_up(incl, o);
-      if (lane >= o) incl += up;
+// Sum over the lanes up to and including this one: six additions across lanes.
+__device__ __forceinline__ int wave_prefix(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false);   // row_shr 1, 2, 4, 8
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);   // row_bcast 15 into rows 1 and 3, 31 into 2 and 3
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);
+  return x;
+}
+__device__ __forceinline__ int wave_total(int x) { return __builtin_amdgcn_readlane(wave_prefix(x), 63); }
+
+// A workgroup's row tile: its sequence, the tile's number in it, and the sequence's rows in both tensors.
+struct TilePlace {
+  int b, tile;
+  SeqRows own, other;
+};
+
+// Tile t in the order in which workgroups take them.  All lanes of a wavefront look together.  Up to 64 sequences: the tiles
+// with the most work first, whatever their sequence (work in tiles of the other side: with `causal` tile k of queries has k and the
+// keys that were there before, tile k of keys, FROM_END, what is left behind it; without, every tile all rows of the other side).  More:
+// sequence by sequence, with `causal` from the tile with the most work on.
+template <bool FROM_END>
+__device__ __forceinline__ bool find_tile(const int32_t* cu_own, const int32_t* cu_other, int B, int Town, int Tother, int shift, bool causal,
+                                          int t, TilePlace& p) {
+  const int lane = threadIdx.x & 63, round = (1 << shift) - 1;
+  if (B > 64) {
+    int before = 0;
+    for (int b0 = 0; b0 < B; b0 += 64) {
+      const int n = b0 + lane < B ? (seq_rows(cu_own, b0 + lane, Town).n + round) >> shift : 0;
+      const int incl = wave_prefix(n), total = __builtin_amdgcn_readlane(incl, 63);
+      if (t - before < total) {
+        const int src = __builtin_ctzll(__ballot(incl > t - before));
+        const int k = t - before - (src > 0 ? __builtin_amdgcn_readlane(incl, src - 1) : 0);
+        p.b = b0 + src;
+        p.tile = FROM_END ? k : __builtin_amdgcn_readlane(n, src) - 1 - k;
+        p.own = seq_rows(cu_own, p.b, Town);
+        p.other = seq_rows(cu_other, p.b, Tother);
+        return true;
+      }
+      before += total;
     }
-    const int total = __builtin_amdgcn_readlane(incl, 63);
-    if (t - before < total) {
-      const int src = __builtin_ctzll(__ballot(incl > t - before));
-      b = b0 + src;
-      s = {__builtin_amdgcn_readlane(x.first, src), __builtin_amdgcn_readlane(x.n, src)};
-      tile = t - before - (src > 0 ? __builtin_amdgcn_readlane(incl, src - 1) : 0);
-      return true;
-    }
-    before += total;
+    return false;
   }
-  return false;
+  SeqRows own = {0, 0}, other = {0, 0};
+  if (lane < B) {
+    own = seq_rows(cu_own, lane, Town);
+    other = seq_rows(cu_other, lane, Tother);
+  }
+  const int n = (own.n + round) >> shift;
+  const int base = !causal ? other.n >> shift : FROM_END ? 0 : max(0, other.n - own.n) >> shift;
+  // tiles of the lane's sequence with work of at least x + 1
+  auto count = [&](int x) { return causal ? min(max(base + n - x, 0), n) : base >= x ? n : 0; };
+  int lo = 0, hi = 1, above = 0;                           // total(lo) > t >= total(hi)
+  if (wave_total(n) <= t) return false;
+  if (B == 1) {
+    p.tile = causal ? __builtin_amdgcn_readfirstlane(n) - 1 - t : t;
+    p.b = 0;
+  } else {
+    for (; wave_total(count(hi)) > t; hi *= 2) lo = hi;
+    while (hi - lo > 1) {
+      const int mid = lo + (hi - lo) / 2;
+      if (wave_total(count(mid)) > t) lo = mid;
+      else hi = mid;
+    }
+    above = wave_total(count(hi));
+    const int incl = wave_prefix(count(lo) - count(hi));
+    p.b = __builtin_ctzll(__ballot(incl > t - above));
+    p.tile = causal ? lo - __builtin_amdgcn_readlane(base, p.b) : t - above - (p.b > 0 ? __builtin_amdgcn_readlane(incl, p.b - 1) : 0);
+  }
+  if (FROM_END && causal) p.tile = __builtin_amdgcn_readlane(n, p.b) - 1 - p.tile;
+  p.own = {__builtin_amdgcn_readlane(own.first, p.b), __builtin_amdgcn_readlane(own.n, p.b)};
+  p.other = {__builtin_amdgcn_readlane(other.first, p.b), __builtin_amdgcn_readlane(other.n, p.b)};
+  return true;
 }
 
-// Workgroup id -> place in a list that the eight XCDs (workgroup id mod 8) share in contiguous parts.
-__device__ __forceinline__ int xcd_contiguous(int id, int total) {
-  const int q = total >> 3, r = total & 7, x = id & 7;
-  return x * q + min(x, r) + (id >> 3);
+// Workgroups over (key head, item): all items of a key head, which read the same keys and values, on one XCD (workgroup id mod 8) where
+// the heads are a multiple of eight, on as few XCDs as there are for each where they divide eight, and the items of all heads of an XCD
+// in order.
+struct HeadItem { int hk, item; };
+inline int head_item_grid(int Hk, int items) { return Hk % 8 == 0 || 8 % Hk != 0 ? Hk * items : (int)(((int64_t)items * Hk + 7) / 8 * 8); }
+__device__ __forceinline__ HeadItem head_item(int id, int Hk) {
+  if (Hk % 8 == 0) {
+    const int per = Hk >> 3, j = id >> 3;
+    return {(id & 7) * per + j % per, j / per};
+  }
+  if (8 % Hk == 0) return {(id & 7) % Hk, (id >> 3) * (8 / Hk) + (id & 7) / Hk};   // (may be one of the few past the last)
+  return {id % Hk, id / Hk};
 }
 
 // 16-byte chunk of a tile of rows of RB bytes in LDS: chunk c of row r sits at c ^ chunk_swizzle(r).  Sixteen rows at one

@@ -21,7 +21,6 @@ struct FwdArgs {
   const int32_t *cu_q, *cu_k;
   float* lse;
   int B, Tq, Tk, Hk, G, hshift;   // G = H / Hk, 1 << hshift heads of a group in a workgroup
-  int tiles, units;               // tiles of positions at most, workgroups
   int causal;
   float c;
 };
@@ -60,15 +59,13 @@ __global__ __launch_bounds__(256, 2) void prompt_fwd_kernel(const FwdArgs a) {
   __shared__ __align__(256) char smem[4 * TILE_BYTES];   // K, V, twice
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 31, h = lane >> 5;
 
-  const int hsets = a.G >> a.hshift, unit = xcd_contiguous(blockIdx.x, a.units);
-  const int hk = unit / (hsets * a.tiles), rest = unit - hk * (hsets * a.tiles);
-  // (the tiles that see the most keys first)
-  const int t_all = a.tiles - 1 - rest / hsets, hs = rest % hsets;
-  const int pshift = 7 - a.hshift;                       // positions of a workgroup
-  int b, tile;
-  SeqRows sq;
-  if (!find_tile(a.cu_q, a.B, a.Tq, pshift, t_all, b, tile, sq)) return;
-  const SeqRows sk = seq_rows(a.cu_k, b, a.Tk);
+  const int hsets = a.G >> a.hshift, pshift = 7 - a.hshift;               // 1 << pshift positions of a workgroup
+  const HeadItem w = head_item(blockIdx.x, a.Hk);
+  const int hk = w.hk, hs = w.item % hsets;
+  TilePlace at;
+  if (!find_tile<false>(a.cu_q, a.cu_k, a.B, a.Tq, a.Tk, pshift, a.causal, w.item / hsets, at)) return;
+  const int tile = at.tile;
+  const SeqRows sq = at.own, sk = at.other;
   const int nq = sq.n, nk = sk.n, ahead = nk - nq;       // query i sees keys up to i + ahead
   const int head = hk * a.G + (hs << a.hshift) + (wave & ((1 << a.hshift) - 1));
   const int p0 = (tile << pshift), i0 = p0 + (wave >> a.hshift) * 32;
@@ -212,9 +209,9 @@ int check_attn(const spt_attn_shape_t* s) {
   if (s->B < 1 || s->Tq < 1 || s->Tk < 1 || s->H < 1 || s->Hk < 1 || s->dh < 1 || s->H % s->Hk != 0) return SPT_ERR_ARG;
   if (s->causal != 0 && s->causal != 1) return SPT_ERR_ARG;
   if (!isfinite(s->scale) || !(s->scale > 0.f)) return SPT_ERR_ARG;
-  if ((s->dh != 64 && s->dh != 128) || s->B > 65535 || s->H > 65535) return SPT_ERR_UNSUPPORTED;
-  // (workgroups: tiles of 32 rows at least, in every sequence, times heads)
-  if (((int64_t)s->Tq / 32 + s->B) * s->H > INT_MAX || ((int64_t)s->Tk / 32 + s->B) * s->H > INT_MAX) return SPT_ERR_UNSUPPORTED;
+  if ((s->dh != 64 && s->dh != 128) || s->B > 4096 || s->H > 65535) return SPT_ERR_UNSUPPORTED;
+  // (workgroups: tiles of 32 rows at least, in every sequence, times heads, and a few)
+  if (((int64_t)s->Tq / 32 + s->B) * s->H > INT_MAX - 8 || ((int64_t)s->Tk / 32 + s->B) * s->H > INT_MAX - 8) return SPT_ERR_UNSUPPORTED;
   return SPT_OK;
 }
 
@@ -238,13 +235,12 @@ extern "C" int spt_attn_prompt_fwd(const spt_attn_shape_t* shape, const void* Q,
   a.cu_q = cu_q; a.cu_k = cu_k; a.lse = lse;
   a.B = s.B; a.Tq = s.Tq; a.Tk = s.Tk; a.Hk = s.Hk; a.G = s.H / s.Hk;
   a.hshift = attn_heads_shift(a.G);
-  a.tiles = (int)(((int64_t)s.Tq >> (7 - a.hshift)) + s.B);
-  a.units = a.tiles * s.Hk * (a.G >> a.hshift);
+  const int grid = head_item_grid(s.Hk, ((s.Tq >> (7 - a.hshift)) + s.B) * (a.G >> a.hshift));   // (tiles: so many at most)
   a.causal = s.causal;
   a.c = s.scale * kLog2e;
   const hipStream_t st = static_cast<hipStream_t>(stream);
   ScopedKernelTimer timer(kSlotAttnFwd, st);
-  if (s.dh == 128) hipLaunchKernelGGL(prompt_fwd_kernel<128>, dim3(a.units), dim3(256), 0, st, a);
-  else hipLaunchKernelGGL(prompt_fwd_kernel<64>, dim3(a.units), dim3(256), 0, st, a);
+  if (s.dh == 128) hipLaunchKernelGGL(prompt_fwd_kernel<128>, dim3(grid), dim3(256), 0, st, a);
+  else hipLaunchKernelGGL(prompt_fwd_kernel<64>, dim3(grid), dim3(256), 0, st, a);
   return hipGetLastError() == hipSuccess ? SPT_OK : SPT_ERR_HIP;
 }

@@ -26,7 +26,6 @@ struct BwdArgs {
   const float* lse;
   float *off, *neg_d;             // [H][Tq]: row_offset(lse), -D
   int B, Tq, Tk, Hk, G, hshift;
-  int tiles, units;               // of the launch
   int causal;
   float c, scale;
 };
@@ -85,14 +84,13 @@ __global__ __launch_bounds__(256, 2) void prompt_bwd_q_kernel(const BwdArgs a) {
   constexpr bool OWN = DH == 128;
   __shared__ __align__(256) char smem[(kRing * 2 + (OWN ? 4 : 0)) * TILE_BYTES];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 31, h = lane >> 5;
-  const int hsets = a.G >> a.hshift, unit = xcd_contiguous(blockIdx.x, a.units);
-  const int hk = unit / (hsets * a.tiles), rest = unit - hk * (hsets * a.tiles);
-  const int t_all = a.tiles - 1 - rest / hsets, hs = rest % hsets;
-  const int pshift = 7 - a.hshift;
-  int b, tile;
-  SeqRows sq;
-  if (!find_tile(a.cu_q, a.B, a.Tq, pshift, t_all, b, tile, sq)) return;
-  const SeqRows sk = seq_rows(a.cu_k, b, a.Tk);
+  const int hsets = a.G >> a.hshift, pshift = 7 - a.hshift;
+  const HeadItem w = head_item(blockIdx.x, a.Hk);
+  const int hk = w.hk, hs = w.item % hsets;
+  TilePlace at;
+  if (!find_tile<false>(a.cu_q, a.cu_k, a.B, a.Tq, a.Tk, pshift, a.causal, w.item / hsets, at)) return;
+  const int tile = at.tile;
+  const SeqRows sq = at.own, sk = at.other;
   const int nq = sq.n, nk = sk.n, ahead = nk - nq;
   const int head = hk * a.G + (hs << a.hshift) + (wave & ((1 << a.hshift) - 1));
   const int p0 = (tile << pshift), i0 = p0 + (wave >> a.hshift) * 32;
@@ -272,11 +270,12 @@ __global__ __launch_bounds__(256, 2) void prompt_bwd_kv_kernel(const BwdArgs a) 
   __shared__ __align__(256) char smem[(kRing * 2 + (OWN ? 4 : 0)) * TILE_BYTES];   // Q, dY
   __shared__ __align__(256) float stat[kRing][64];               // a tile's rows' offsets and -D
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 31, h = lane >> 5;
-  const int unit = xcd_contiguous(blockIdx.x, a.units), hk = unit / a.tiles;
-  int b, tile;
-  SeqRows sk;
-  if (!find_tile(a.cu_k, a.B, a.Tk, 7, unit - hk * a.tiles, b, tile, sk)) return;
-  const SeqRows sq = seq_rows(a.cu_q, b, a.Tq);
+  const HeadItem w = head_item(blockIdx.x, a.Hk);
+  const int hk = w.hk;
+  TilePlace place;
+  if (!find_tile<true>(a.cu_k, a.cu_q, a.B, a.Tk, a.Tq, 7, a.causal, w.item, place)) return;
+  const int tile = place.tile;
+  const SeqRows sk = place.own, sq = place.other;
   const int nq = sq.n, nk = sk.n, ahead = nk - nq;
   const int j0 = tile * kOwnKeys + wave * 32, mine = min(j0 + i, nk - 1);
   const int first = a.causal ? max(0, mine - ahead) : 0;                 // the first query that sees the lane's key
@@ -462,16 +461,14 @@ extern "C" int spt_attn_prompt_bwd(const spt_attn_shape_t* shape, const void* Q,
   const hipStream_t st = static_cast<hipStream_t>(stream);
   {
     ScopedKernelTimer timer(kSlotAttnBwdQ, st);
-    a.tiles = (int)(((int64_t)s.Tq >> (7 - a.hshift)) + s.B);
-    a.units = a.tiles * s.Hk * (a.G >> a.hshift);
-    if (s.dh == 128) hipLaunchKernelGGL(prompt_bwd_q_kernel<128>, dim3(a.units), dim3(256), 0, st, a);
-    else hipLaunchKernelGGL(prompt_bwd_q_kernel<64>, dim3(a.units), dim3(256), 0, st, a);
+    const int grid = head_item_grid(s.Hk, ((s.Tq >> (7 - a.hshift)) + s.B) * (a.G >> a.hshift));
+    if (s.dh == 128) hipLaunchKernelGGL(prompt_bwd_q_kernel<128>, dim3(grid), dim3(256), 0, st, a);
+    else hipLaunchKernelGGL(prompt_bwd_q_kernel<64>, dim3(grid), dim3(256), 0, st, a);
     if (hipGetLastError() != hipSuccess) return SPT_ERR_HIP;
   }
   ScopedKernelTimer timer(kSlotAttnBwdKV, st);
-  a.tiles = s.Tk / kOwnKeys + s.B;
-  a.units = a.tiles * s.Hk;
-  if (s.dh == 128) hipLaunchKernelGGL(prompt_bwd_kv_kernel<128>, dim3(a.units), dim3(256), 0, st, a);
-  else hipLaunchKernelGGL(prompt_bwd_kv_kernel<64>, dim3(a.units), dim3(256), 0, st, a);
+  const int grid = head_item_grid(s.Hk, s.Tk / kOwnKeys + s.B);
+  if (s.dh == 128) hipLaunchKernelGGL(prompt_bwd_kv_kernel<128>, dim3(grid), dim3(256), 0, st, a);
+  else hipLaunchKernelGGL(prompt_bwd_kv_kernel<64>, dim3(grid), dim3(256), 0, st, a);
   return hipGetLastError() == hipSuccess ? SPT_OK : SPT_ERR_HIP;
 }
