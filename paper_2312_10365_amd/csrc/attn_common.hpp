@@ -211,13 +211,16 @@ __device__ __forceinline__ bf16x8 pack8(const float* x) {
   return as_bf16x8(u32x4{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7])});
 }
 
-// Whether one of eight bf16 is infinite or NaN.
-__device__ __forceinline__ bool any_not_finite(u32x4 x) {
-  bool bad = false;
+// Whether any of the bf16 looked at was infinite or NaN: the largest magnitude, two halves at a time.
+struct NotFinite {
+  typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+  u16x2 top = {0, 0};
+  __device__ __forceinline__ void look(u32x4 x) {
 #pragma unroll
-  for (int e = 0; e < 4; ++e) bad |= (x[e] & 0x7F80u) == 0x7F80u || (x[e] & 0x7F800000u) == 0x7F800000u;
-  return bad;
-}
+    for (int e = 0; e < 4; ++e) top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, x[e] & 0x7FFF7FFFu));
+  }
+  __device__ __forceinline__ bool found() const { return top[0] >= 0x7F80 || top[1] >= 0x7F80; }
+};
 
 __device__ __forceinline__ float wave_sum(float x) {
 #pragma unroll

@@ -76,6 +76,7 @@ __global__ __launch_bounds__(256, 2) void prompt_fwd_kernel(const FwdArgs a) {
   const int mine = min(i0 + i, nq - 1);
   const int seen = a.causal ? min(nk, mine + ahead + 1) : nk;            // keys the lane's query sees (may be negative)
   const int ntile = kend > 0 ? (kend + kTileKeys - 1) / kTileKeys : 0;
+  const int full = max(0, a.causal ? min(nk, p0 + ahead + 1) : nk);     // keys that all queries of the workgroup see
 
   const char* qrow = a.Q.p + (int64_t)(sq.first + mine) * a.Q.row + (int64_t)head * a.Q.head;
   bf16x8 qf[KS];
@@ -108,7 +109,7 @@ __global__ __launch_bounds__(256, 2) void prompt_fwd_kernel(const FwdArgs a) {
 #pragma unroll
     for (int r = 0; r < 16; ++r) o[d][r] = 0.f;
   float m = -INFINITY, neg_m = 0.f, l = 0.f;
-  bool bad = false;
+  NotFinite not_finite;
 
   if (ntile > 0) fetch(0, 0);
   for (int t = 0; t < ntile; ++t) {
@@ -116,8 +117,12 @@ __global__ __launch_bounds__(256, 2) void prompt_fwd_kernel(const FwdArgs a) {
     __syncthreads();
     if (t + 1 < ntile) fetch(t + 1, (t + 1) & 1);
     const int j0 = t * kTileKeys;
-    if (j0 >= wave_kend) continue;
     const uint32_t kt_ = tiles + (t & 1) * 2 * TILE_BYTES, vt_ = kt_ + TILE_BYTES;
+    if (j0 + kTileKeys > full) {
+#pragma unroll
+      for (int u = 0; u < TILE_BYTES / 4096; ++u) not_finite.look(lds_read<u32x4>(vt_ + u * 4096 + threadIdx.x * 16));
+    }
+    if (j0 >= wave_kend) continue;
     lds.fresh();
     f32x16 s[2];
 #pragma unroll
@@ -134,9 +139,6 @@ __global__ __launch_bounds__(256, 2) void prompt_fwd_kernel(const FwdArgs a) {
       for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
         for (int r = 0; r < 16; ++r) s[kt][r] = 32 * kt + 8 * (r >> 2) + (r & 3) < left ? s[kt][r] : -INFINITY;
-      // rows of V that some query must not see: 0 times an infinity is NaN
-#pragma unroll
-      for (int u = 0; u < TILE_BYTES / 1024; ++u) bad |= any_not_finite(lds_read<u32x4>(vt_ + u * 1024 + lane * 16));
     }
     float top = s[0][0];
 #pragma unroll
@@ -176,7 +178,8 @@ __global__ __launch_bounds__(256, 2) void prompt_fwd_kernel(const FwdArgs a) {
   }
 
   float* lse = a.lse ? a.lse + (int64_t)head * a.Tq + sq.first : nullptr;
-  if (__any(bad)) {
+  // rows of V that not all queries may see hold infinities or NaN: 0 times those is NaN
+  if (full < ntile * kTileKeys && __syncthreads_or(not_finite.found())) {
     for (int r = 0; r < min(32, nq - i0); ++r) {
       const int row = i0 + r;
       slow_row<DH>(a.Q.p + (int64_t)(sq.first + row) * a.Q.row + (int64_t)head * a.Q.head, kbase, a.K.row, vbase, a.V.row,

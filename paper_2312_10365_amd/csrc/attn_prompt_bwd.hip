@@ -45,13 +45,13 @@ __device__ __forceinline__ PairGrad pair_grad(const char* q, const char* k, cons
 
 // Rows q0 .. q0 + 31 of two tensors of n rows into a pair of tiles (rows past the end: the last one again).
 template <int DH>
-__device__ __forceinline__ void fetch_pair(const char* x, int64_t xrow, const char* y, int64_t yrow, int q0, int n, const char* tiles, int wave) {
+__device__ __forceinline__ void fetch_pair(int tid, const char* x, int64_t xrow, const char* y, int64_t yrow, int q0, int n, const char* tiles, int wave) {
   constexpr int COPIES = kTile * (DH / 8) / 256;
   const char* xb = x + q0 * xrow;
   const char* yb = y + q0 * yrow;
 #pragma unroll
   for (int u = 0; u < COPIES; ++u) {
-    const int slot = u * 256 + (int)threadIdx.x, r0 = slot / (DH / 8);
+    const int slot = u * 256 + tid, r0 = slot / (DH / 8);
     const uint32_t chunk = ((slot % (DH / 8)) ^ row_swizzle<DH>(r0)) * 16, r = (uint32_t)min(r0, n - 1 - q0);
     const uint32_t at = lds_addr(tiles + u * 4096 + wave * 1024);
     dma16_at(xb, r * (uint32_t)xrow + chunk, at);
@@ -101,10 +101,11 @@ __global__ __launch_bounds__(256, 2) void prompt_bwd_q_kernel(const BwdArgs a) {
   const int mine = min(i0 + i, nq - 1);
   const int seen = a.causal ? min(nk, mine + ahead + 1) : nk;
   const int ntile = kend > 0 ? (kend + kTile - 1) / kTile : 0;
+  const int full = max(0, a.causal ? min(nk, p0 + ahead + 1) : nk);     // keys that all queries of the workgroup see
 
   const char* kbase = a.K.p + (int64_t)sk.first * a.K.row + (int64_t)hk * a.K.head;
   const char* vbase = a.V.p + (int64_t)sk.first * a.V.row + (int64_t)hk * a.V.head;
-  auto fetch = [&](int t) { fetch_pair<DH>(kbase, a.K.row, vbase, a.V.row, t * kTile, nk, smem + t % kRing * 2 * TILE_BYTES, wave); };
+  auto fetch = [&](int t) { fetch_pair<DH>(threadIdx.x, kbase, a.K.row, vbase, a.V.row, t * kTile, nk, smem + t % kRing * 2 * TILE_BYTES, wave); };
   if (ntile > 0) fetch(0);
 
   const int64_t row = sq.first + mine;
@@ -133,7 +134,7 @@ __global__ __launch_bounds__(256, 2) void prompt_bwd_q_kernel(const BwdArgs a) {
 #pragma unroll
     for (int r = 0; r < 16; ++r) o[d][r] = mean[d][r] = 0.f;
   float left_over = 0.f;                                 // sum of dS: what D lacks
-  bool bad = false;
+  NotFinite not_finite;
 
   auto first_products = [&](int t, f32x16& s, f32x16& dp) {
     const uint32_t kt = tiles + (t % kRing) * 2 * TILE_BYTES;
@@ -191,19 +192,20 @@ __global__ __launch_bounds__(256, 2) void prompt_bwd_q_kernel(const BwdArgs a) {
   for (int t = 0; t < ntile; ++t) {
     turn(t);
     const int j0 = t * kTile;
+    if (j0 + kTile > full) {
+#pragma unroll
+      for (int u = 0; u < TILE_BYTES / 4096; ++u) not_finite.look(lds_read<u32x4>(tiles + t % kRing * 2 * TILE_BYTES + u * 4096 + threadIdx.x * 16));
+    }
     if (j0 >= wave_kend) continue;
     const bool masked = j0 + kTile > wave_full;
-    if (masked) {
-#pragma unroll
-      for (int u = 0; u < TILE_BYTES / 1024; ++u) bad |= any_not_finite(lds_read<u32x4>(tiles + (t % kRing) * 2 * TILE_BYTES + u * 1024 + lane * 16));
-    }
     f32x16 s, dp;
     first_products(t, s, dp);
     second_products(t, weights(t, s, dp, masked));
   }
   left_over += other_half(left_over);
   const int64_t stat = (int64_t)head * a.Tq;
-  if (__any(bad)) {
+  // rows that not all queries may see hold infinities or NaN: 0 times those is NaN
+  if (full < ntile * kTile && __syncthreads_or(not_finite.found())) {
     for (int r = 0; r < min(32, nq - i0); ++r) {
       const int64_t at = sq.first + i0 + r;
       const float Dr = __shfl(D, r), offr = __shfl(off, r);
@@ -263,13 +265,26 @@ __device__ __forceinline__ void slow_dkv_row(const BwdArgs& a, const SeqRows& sq
   }
 }
 
-template <int DH>
-__global__ __launch_bounds__(256, 2) void prompt_bwd_kv_kernel(const BwdArgs a) {
-  constexpr int KS = DH / 16, DT = DH / 32, TILE_BYTES = kTile * DH * 2;
-  constexpr bool OWN = DH == 128;                                // V of the wavefront's keys stays in LDS, as above
-  __shared__ __align__(256) char smem[(kRing * 2 + (OWN ? 4 : 0)) * TILE_BYTES];   // Q, dY
-  __shared__ __align__(256) float stat[kRing][64];               // a tile's rows' offsets and -D
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 31, h = lane >> 5;
+// Sizes of the key side: GROUPS groups of four wavefronts go through every GROUPS-th step, on the same 128 keys.
+template <int DH, int GROUPS>
+struct KvSizes {
+  static constexpr int TILE_BYTES = kTile * DH * 2, STAT = 256;
+  static constexpr bool OWN = DH == 128;                         // V of the keys stays in LDS: registers, as above
+  static constexpr int RING = kRing * (2 * TILE_BYTES + STAT);   // of a group: tiles of Q and dY, their rows' offsets and -D
+  static constexpr int SMEM = GROUPS * RING + (OWN ? 4 * TILE_BYTES : 0);
+  static_assert(GROUPS == 1 || SMEM >= 4 * DH * 32 * 4, "a gradient of the second group passes through LDS");
+};
+
+template <int DH, int GROUPS>
+__global__ __launch_bounds__(256 * GROUPS, 2) void prompt_bwd_kv_kernel(const BwdArgs a) {
+  typedef KvSizes<DH, GROUPS> Sizes;
+  constexpr int KS = DH / 16, DT = DH / 32, TILE_BYTES = Sizes::TILE_BYTES;
+  constexpr bool OWN = Sizes::OWN;
+  extern __shared__ __align__(256) char smem[];
+  const int lane = threadIdx.x & 63, i = lane & 31, h = lane >> 5, tid = threadIdx.x & 255;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) & 3, group = GROUPS == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 8);
+  char* ring = smem + group * Sizes::RING;
+  float* stats = reinterpret_cast<float*>(ring + kRing * 2 * TILE_BYTES);
   const HeadItem w = head_item(blockIdx.x, a.Hk);
   const int hk = w.hk;
   TilePlace place;
@@ -295,41 +310,43 @@ __global__ __launch_bounds__(256, 2) void prompt_bwd_kv_kernel(const BwdArgs a) 
     return t + 1 == masked_steps ? Place{0, 0} : Place{p.g + 1, 0};
   };
   auto fetch = [&](int t, const Place& p) {
-    const int head = hk * a.G + p.g, q0 = first_query(t, p), buf = t % kRing;
-    fetch_pair<DH>(a.Q.p + (int64_t)sq.first * a.Q.row + (int64_t)head * a.Q.head, a.Q.row,
-                   a.dY.p + (int64_t)sq.first * a.dY.row + (int64_t)head * a.dY.head, a.dY.row, q0, nq, smem + buf * 2 * TILE_BYTES, wave);
+    const int head = hk * a.G + p.g, q0 = first_query(t, p), buf = t / GROUPS % kRing;
+    fetch_pair<DH>(tid, a.Q.p + (int64_t)sq.first * a.Q.row + (int64_t)head * a.Q.head, a.Q.row,
+                   a.dY.p + (int64_t)sq.first * a.dY.row + (int64_t)head * a.dY.head, a.dY.row, q0, nq, ring + buf * 2 * TILE_BYTES, wave);
     const int64_t at = (int64_t)head * a.Tq + sq.first + q0 + min(i, nq - 1 - q0);
-    if (wave == 0) dma4(h ? a.neg_d + at : a.off + at, lds_addr(stat[buf]));
+    if (wave == 0) dma4(h ? a.neg_d + at : a.off + at, lds_addr(stats + buf * 64));
   };
-  Place coming = {0, 0};                                                 // of the last step asked for
-  if (steps > 0) fetch(0, coming);
+  // the group's steps: group, group + GROUPS, ...
+  Place here = {0, 0}, coming;
+  if (group == 1) here = after(0, here);
+  coming = here;
+  if (group < steps) fetch(group, here);
 
   const char* krow = a.K.p + (int64_t)(sk.first + mine) * a.K.row + (int64_t)hk * a.K.head;
   const char* vrow = a.V.p + (int64_t)(sk.first + mine) * a.V.row + (int64_t)hk * a.V.head;
   bf16x8 kf[KS], vf[OWN ? 1 : KS];
   TileReader<DH> lds(lane);
-  const uint32_t tiles = lds_addr(smem), own = tiles + (kRing * 2 + wave) * TILE_BYTES;
+  const uint32_t tiles = lds_addr(ring), own = lds_addr(smem) + GROUPS * Sizes::RING + wave * TILE_BYTES;
 #pragma unroll
   for (int s = 0; s < KS; ++s) {
     kf[s] = *reinterpret_cast<const bf16x8*>(krow + s * 32 + h * 16);
     const bf16x8 v = *reinterpret_cast<const bf16x8*>(vrow + s * 32 + h * 16);
-    if (OWN) *reinterpret_cast<bf16x8*>(smem + (kRing * 2 + wave) * TILE_BYTES + (lds.row ^ (uint32_t)(s * 32))) = v;
-    else vf[s] = v;
+    if (!OWN) vf[s] = v;
+    else if (group == 0) *reinterpret_cast<bf16x8*>(smem + GROUPS * Sizes::RING + wave * TILE_BYTES + (lds.row ^ (uint32_t)(s * 32))) = v;
   }
   f32x16 ok[DT], ov[DT];
 #pragma unroll
   for (int d = 0; d < DT; ++d)
 #pragma unroll
     for (int r = 0; r < 16; ++r) ok[d][r] = ov[d][r] = 0.f;
-  bool bad = false;
+  NotFinite not_finite;
 
-  auto first_products = [&](int t, f32x16& s, f32x16& dp) {
-    const int buf = t % kRing;
+  auto first_products = [&](int buf, f32x16& s, f32x16& dp) {
     const uint32_t qt = tiles + buf * 2 * TILE_BYTES;
     lds.fresh();
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-      const f32x4 d = *reinterpret_cast<const f32x4*>(stat[buf] + 32 + 8 * q + 4 * h);   // (dP starts from -D)
+      const f32x4 d = *reinterpret_cast<const f32x4*>(stats + buf * 64 + 32 + 8 * q + 4 * h);   // (dP starts from -D)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         s[4 * q + e] = 0.f;
@@ -342,10 +359,10 @@ __global__ __launch_bounds__(256, 2) void prompt_bwd_kv_kernel(const BwdArgs a) 
     for (int ks = 0; ks < KS; ++ks)
       dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lds.rows(qt + TILE_BYTES, 0, ks), OWN ? lds.rows(own, 0, ks) : vf[OWN ? 0 : ks], dp, 0, 0, 0);
   };
-  auto weights = [&](int t, int q0, f32x16& s, f32x16& dp, bool masked) {
+  auto weights = [&](int buf, int q0, f32x16& s, f32x16& dp, bool masked) {
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-      const f32x4 off = *reinterpret_cast<const f32x4*>(stat[t % kRing] + 8 * q + 4 * h);
+      const f32x4 off = *reinterpret_cast<const f32x4*>(stats + buf * 64 + 8 * q + 4 * h);
 #pragma unroll
       for (int e = 0; e < 4; ++e) s[4 * q + e] = fmaf(s[4 * q + e], a.c, -off[e]);
     }
@@ -368,8 +385,8 @@ __global__ __launch_bounds__(256, 2) void prompt_bwd_kv_kernel(const BwdArgs a) 
     }
     return w;
   };
-  auto second_products = [&](int t, const Weights& w) {
-    const uint32_t qt = tiles + t % kRing * 2 * TILE_BYTES;
+  auto second_products = [&](int buf, const Weights& w) {
+    const uint32_t qt = tiles + buf * 2 * TILE_BYTES;
     lds.fresh();
 #pragma unroll
     for (int half = 0; half < 2; ++half)
@@ -379,38 +396,64 @@ __global__ __launch_bounds__(256, 2) void prompt_bwd_kv_kernel(const BwdArgs a) 
         ok[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lds.columns(qt, half, d), as_bf16x8(w.ds[half]), ok[d], 0, 0, 0);
       }
   };
-  auto turn = [&](int t) {                                               // step t's tile is there; asks for the next
-    wait_vmcnt<0>();
+  for (int t0 = 0; t0 < steps; t0 += GROUPS) {
+    wait_vmcnt<0>();                                                     // the step's tiles are there; asks for the next one's
     __syncthreads();
-    if (t + 1 < steps) {
-      coming = after(t, coming);
-      fetch(t + 1, coming);
+    const int t = t0 + group, buf = t0 / GROUPS % kRing;
+    if (t + GROUPS < steps) {
+#pragma unroll
+      for (int n = 0; n < GROUPS; ++n) coming = after(t + n, coming);
+      fetch(t + GROUPS, coming);
     }
-  };
-  Place here = {0, 0};
-  for (int t = 0; t < steps; ++t) {
-    turn(t);
+    if (t >= steps) continue;
     const int q0 = first_query(t, here);
-    here = after(t, here);
-    if (q0 < wave_begin) continue;
+    here = coming;
     const bool masked = t < masked_steps;
     if (masked) {
 #pragma unroll
-      for (int u = 0; u < 2 * TILE_BYTES / 1024; ++u)
-        bad |= any_not_finite(lds_read<u32x4>(tiles + t % kRing * 2 * TILE_BYTES + u * 1024 + lane * 16));
+      for (int u = 0; u < 2 * TILE_BYTES / 4096; ++u) not_finite.look(lds_read<u32x4>(tiles + buf * 2 * TILE_BYTES + u * 4096 + tid * 16));
     }
+    if (q0 < wave_begin) continue;
     f32x16 s, dp;
-    first_products(t, s, dp);
-    second_products(t, weights(t, q0, s, dp, masked));
+    first_products(buf, s, dp);
+    second_products(buf, weights(buf, q0, s, dp, masked));
   }
-  if (__any(bad)) {
-    for (int r = 0; r < min(32, nk - j0); ++r) {
+  // rows that not all keys may see hold infinities or NaN: 0 times those is NaN
+  if (masked_steps > 0 && __syncthreads_or(not_finite.found())) {
+    for (int r = group; r < min(32, nk - j0); r += GROUPS) {
       const int64_t at = sk.first + j0 + r;
       slow_dkv_row<DH>(a, sq, hk, a.causal ? max(0, j0 + r - ahead) : 0, a.K.p + at * a.K.row + (int64_t)hk * a.K.head,
                        a.V.p + at * a.V.row + (int64_t)hk * a.V.head, a.dK.p + at * a.dK.row + (int64_t)hk * a.dK.head,
                        a.dV.p + at * a.dV.row + (int64_t)hk * a.dV.head);
     }
     return;
+  }
+  if (GROUPS == 2) {                                                     // the second group's sums, one gradient at a time
+    float* half = reinterpret_cast<float*>(smem) + wave * (DT * 1024) + lane * 4;
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+      f32x16* sum = n == 0 ? ok : ov;
+      __syncthreads();
+      if (group == 1) {
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            *reinterpret_cast<f32x4*>(half + (d * 4 + q) * 256) = f32x4{sum[d][4 * q], sum[d][4 * q + 1], sum[d][4 * q + 2], sum[d][4 * q + 3]};
+      }
+      __syncthreads();
+      if (group == 0) {
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const f32x4 x = *reinterpret_cast<const f32x4*>(half + (d * 4 + q) * 256);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum[d][4 * q + e] += x[e];
+          }
+      }
+    }
+    if (group == 1) return;
   }
   if (j0 + i >= nk) return;
   char* dk = a.dK.p + (int64_t)(sk.first + mine) * a.dK.row + (int64_t)hk * a.dK.head + h * 32;
@@ -425,6 +468,15 @@ __global__ __launch_bounds__(256, 2) void prompt_bwd_kv_kernel(const BwdArgs a) 
     *reinterpret_cast<bf16x8*>(dv + d * 64) = pack8(y);
     *reinterpret_cast<bf16x8*>(dv + d * 64 + 16) = pack8(y + 8);
   }
+}
+
+template <int DH, int GROUPS>
+hipError_t launch_kv(const BwdArgs& a, int grid, hipStream_t st) {
+  constexpr int smem = KvSizes<DH, GROUPS>::SMEM;
+  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(prompt_bwd_kv_kernel<DH, GROUPS>), hipFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((prompt_bwd_kv_kernel<DH, GROUPS>), dim3(grid), dim3(256 * GROUPS), smem, st, a);
+  return hipGetLastError();
 }
 
 }  // namespace
@@ -468,7 +520,6 @@ extern "C" int spt_attn_prompt_bwd(const spt_attn_shape_t* shape, const void* Q,
   }
   ScopedKernelTimer timer(kSlotAttnBwdKV, st);
   const int grid = head_item_grid(s.Hk, s.Tk / kOwnKeys + s.B);
-  if (s.dh == 128) hipLaunchKernelGGL(prompt_bwd_kv_kernel<128>, dim3(grid), dim3(256), 0, st, a);
-  else hipLaunchKernelGGL(prompt_bwd_kv_kernel<64>, dim3(grid), dim3(256), 0, st, a);
-  return hipGetLastError() == hipSuccess ? SPT_OK : SPT_ERR_HIP;
+  const hipError_t e = s.dh == 128 ? launch_kv<128, 2>(a, grid, st) : launch_kv<64, 1>(a, grid, st);
+  return e == hipSuccess ? SPT_OK : SPT_ERR_HIP;
 }
