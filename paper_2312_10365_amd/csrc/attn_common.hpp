@@ -201,6 +201,52 @@ struct TileReader {
   }
 };
 
+// 32 rows between memory and a wavefront's own tile in LDS, as whole lines (a lane's own row in registers would be 16 bytes
+// of 64 lines an instruction).  In: asynchronous, rows past n: the last one again.  Out: rows past n are left out.
+template <int DH>
+__device__ __forceinline__ void fetch_rows(const char* x, int64_t row, int n, uint32_t tile, int lane) {
+  constexpr int CHUNKS = DH / 8, ROWS = 64 / CHUNKS;
+#pragma unroll
+  for (int u = 0; u < 32 / ROWS; ++u) {
+    const int r = u * ROWS + lane / CHUNKS;
+    dma16_at(x, (uint32_t)min(r, n - 1) * (uint32_t)row + (((uint32_t)lane % CHUNKS) ^ row_swizzle<DH>(r)) * 16, tile + u * 1024);
+  }
+}
+// The same rows by way of registers: lane L holds 16 bytes of rows u ROWS + L / CHUNKS.
+template <int DH>
+struct RowPieces {
+  static constexpr int CHUNKS = DH / 8, ROWS = 64 / CHUNKS, N = 32 / ROWS;
+  u32x4 x[N];
+  __device__ __forceinline__ void load(const char* p, int64_t row, int n, int lane) {
+#pragma unroll
+    for (int u = 0; u < N; ++u) x[u] = *reinterpret_cast<const u32x4*>(p + min(u * ROWS + lane / CHUNKS, n - 1) * row + (lane % CHUNKS) * 16);
+  }
+  __device__ __forceinline__ void put(char* tile, int lane) const {
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+      const int r = u * ROWS + lane / CHUNKS;
+      *reinterpret_cast<u32x4*>(tile + r * (DH * 2) + (((uint32_t)lane % CHUNKS) ^ row_swizzle<DH>(r)) * 16) = x[u];
+    }
+  }
+};
+// 16 adjacent dims of row r, from 16-byte chunk c on.
+template <int DH>
+__device__ __forceinline__ void put_dims(char* tile, int r, int c, bf16x8 lo, bf16x8 hi) {
+  const uint32_t at = r * (DH * 2) + ((uint32_t)c ^ row_swizzle<DH>(r)) * 16;
+  *reinterpret_cast<bf16x8*>(tile + at) = lo;
+  *reinterpret_cast<bf16x8*>(tile + (at ^ 16u)) = hi;
+}
+template <int DH>
+__device__ __forceinline__ void store_rows(const char* tile, char* x, int64_t row, int n, int lane) {
+  constexpr int CHUNKS = DH / 8, ROWS = 64 / CHUNKS;
+#pragma unroll
+  for (int u = 0; u < 32 / ROWS; ++u) {
+    const int r = u * ROWS + lane / CHUNKS;
+    const u32x4 v = *reinterpret_cast<const u32x4*>(tile + u * 1024 + lane * 16);
+    if (r < n) *reinterpret_cast<u32x4*>(x + r * row + (((uint32_t)lane % CHUNKS) ^ row_swizzle<DH>(r)) * 16) = v;
+  }
+}
+
 __device__ __forceinline__ float other_half(float x) {   // the value of the lane 32 away
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
   return __uint_as_float((threadIdx.x & 32) ? r[0] : r[1]);

@@ -78,11 +78,10 @@ __global__ __launch_bounds__(256, 2) void prompt_fwd_kernel(const FwdArgs a) {
   const int ntile = kend > 0 ? (kend + kTileKeys - 1) / kTileKeys : 0;
   const int full = max(0, a.causal ? min(nk, p0 + ahead + 1) : nk);     // keys that all queries of the workgroup see
 
-  const char* qrow = a.Q.p + (int64_t)(sq.first + mine) * a.Q.row + (int64_t)head * a.Q.head;
-  bf16x8 qf[KS];
-#pragma unroll
-  for (int s = 0; s < KS; ++s) qf[s] = *reinterpret_cast<const bf16x8*>(qrow + s * 32 + h * 16);
-
+  // the wavefront's queries, through the second ring buffer: whole lines
+  const char* qbase = a.Q.p + (int64_t)sq.first * a.Q.row + (int64_t)head * a.Q.head;
+  const uint32_t tiles = lds_addr(smem), mine_lds = 2 * TILE_BYTES + wave * (32 * DH * 2);
+  fetch_rows<DH>(qbase + min(i0, nq - 1) * a.Q.row, a.Q.row, max(nq - i0, 1), tiles + mine_lds, lane);
   const char* kbase = a.K.p + (int64_t)sk.first * a.K.row + (int64_t)hk * a.K.head;
   const char* vbase = a.V.p + (int64_t)sk.first * a.V.row + (int64_t)hk * a.V.head;
   // copies: lane L of an instruction fills 16 bytes of row (u 256 + tid) / (DH / 8)
@@ -102,7 +101,6 @@ __global__ __launch_bounds__(256, 2) void prompt_fwd_kernel(const FwdArgs a) {
     }
   };
   TileReader<DH> lds(lane);
-  const uint32_t tiles = lds_addr(smem);
   f32x16 o[DT];
 #pragma unroll
   for (int d = 0; d < DT; ++d)
@@ -112,6 +110,11 @@ __global__ __launch_bounds__(256, 2) void prompt_fwd_kernel(const FwdArgs a) {
   NotFinite not_finite;
 
   if (ntile > 0) fetch(0, 0);
+  bf16x8 qf[KS];
+  if (ntile > 0) wait_vmcnt<2 * COPIES>();
+  else wait_vmcnt<0>();
+#pragma unroll
+  for (int s = 0; s < KS; ++s) qf[s] = lds.rows(tiles + mine_lds, 0, s);
   for (int t = 0; t < ntile; ++t) {
     wait_vmcnt<0>();
     __syncthreads();
@@ -188,19 +191,21 @@ __global__ __launch_bounds__(256, 2) void prompt_fwd_kernel(const FwdArgs a) {
     }
     return;
   }
-  if (i0 + i >= nq) return;
+  if (i0 >= nq) return;
   l += other_half(l);
   const float inv = l == 0.f ? 0.f : 1.f / l;
-  char* y = a.Y.p + (int64_t)(sq.first + mine) * a.Y.row + (int64_t)head * a.Y.head + h * 32;
+  if (lse && h == 0 && i0 + i < nq) lse[mine] = (m + __builtin_amdgcn_logf(l)) * kLn2;
+  // rows out as whole lines, through the ring buffer that the last tile is not in
+  const uint32_t out = (ntile & 1) * 2 * TILE_BYTES + wave * (32 * DH * 2);
 #pragma unroll
   for (int d = 0; d < DT; ++d) {
     float v[16];
 #pragma unroll
     for (int r = 0; r < 16; ++r) v[r] = o[d][r] * inv;
-    *reinterpret_cast<bf16x8*>(y + d * 64) = pack8(v);
-    *reinterpret_cast<bf16x8*>(y + d * 64 + 16) = pack8(v + 8);
+    put_dims<DH>(smem + out, i, 4 * d + 2 * h, pack8(v), pack8(v + 8));
   }
-  if (lse && h == 0) lse[mine] = (m + __builtin_amdgcn_logf(l)) * kLn2;
+  wave_lds_fence();
+  store_rows<DH>(smem + out, a.Y.p + (int64_t)(sq.first + i0) * a.Y.row + (int64_t)head * a.Y.head, a.Y.row, nq - i0, lane);
 }
 
 }  // namespace

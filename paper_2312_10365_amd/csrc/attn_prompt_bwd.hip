@@ -272,7 +272,7 @@ struct KvSizes {
   static constexpr bool OWN = DH == 128;                         // V of the keys stays in LDS: registers, as above
   static constexpr int RING = kRing * (2 * TILE_BYTES + STAT);   // of a group: tiles of Q and dY, their rows' offsets and -D
   static constexpr int SMEM = GROUPS * RING + (OWN ? 4 * TILE_BYTES : 0);
-  static_assert(GROUPS == 1 || SMEM >= 4 * DH * 32 * 4, "a gradient of the second group passes through LDS");
+  static_assert(GROUPS == 1 || GROUPS * RING >= 4 * DH * 32 * 4, "a gradient of the second group passes through LDS");
 };
 
 template <int DH, int GROUPS>
@@ -322,17 +322,35 @@ __global__ __launch_bounds__(256 * GROUPS, 2) void prompt_bwd_kv_kernel(const Bw
   coming = here;
   if (group < steps) fetch(group, here);
 
-  const char* krow = a.K.p + (int64_t)(sk.first + mine) * a.K.row + (int64_t)hk * a.K.head;
-  const char* vrow = a.V.p + (int64_t)(sk.first + mine) * a.V.row + (int64_t)hk * a.V.head;
   bf16x8 kf[KS], vf[OWN ? 1 : KS];
   TileReader<DH> lds(lane);
   const uint32_t tiles = lds_addr(ring), own = lds_addr(smem) + GROUPS * Sizes::RING + wave * TILE_BYTES;
+  char* own_tile = smem + GROUPS * Sizes::RING + wave * TILE_BYTES;
+  if (!OWN) {
+    const char* krow = a.K.p + (int64_t)(sk.first + mine) * a.K.row + (int64_t)hk * a.K.head;
+    const char* vrow = a.V.p + (int64_t)(sk.first + mine) * a.V.row + (int64_t)hk * a.V.head;
 #pragma unroll
-  for (int s = 0; s < KS; ++s) {
-    kf[s] = *reinterpret_cast<const bf16x8*>(krow + s * 32 + h * 16);
-    const bf16x8 v = *reinterpret_cast<const bf16x8*>(vrow + s * 32 + h * 16);
-    if (!OWN) vf[s] = v;
-    else if (group == 0) *reinterpret_cast<bf16x8*>(smem + GROUPS * Sizes::RING + wave * TILE_BYTES + (lds.row ^ (uint32_t)(s * 32))) = v;
+    for (int s = 0; s < KS; ++s) {
+      kf[s] = *reinterpret_cast<const bf16x8*>(krow + s * 32 + h * 16);
+      vf[OWN ? 0 : s] = *reinterpret_cast<const bf16x8*>(vrow + s * 32 + h * 16);
+    }
+  } else {
+    // as whole lines: K and then V through the wavefronts' tiles (the first group fetches K, the last one V; 32 heads of their own
+    // keys, 16 sequences of 512: 203 us with a lane's own row, 174 so; 64-wide heads lose, 164 and 173)
+    const int64_t row0 = sk.first + min(j0, nk - 1);
+    const int own_rows = max(nk - j0, 1);
+    RowPieces<DH> v;
+    if (group == 0) fetch_rows<DH>(a.K.p + row0 * a.K.row + (int64_t)hk * a.K.head, a.K.row, own_rows, own, lane);
+    if (group == GROUPS - 1) v.load(a.V.p + row0 * a.V.row + (int64_t)hk * a.V.head, a.V.row, own_rows, lane);
+    wait_vmcnt<0>();
+    wave_lds_fence();
+    if (GROUPS > 1) __syncthreads();
+#pragma unroll
+    for (int s = 0; s < KS; ++s) kf[s] = lds.rows(own, 0, s);
+    wave_lds_fence();
+    if (GROUPS > 1) __syncthreads();
+    if (group == GROUPS - 1) v.put(own_tile, lane);
+    wave_lds_fence();
   }
   f32x16 ok[DT], ov[DT];
 #pragma unroll
@@ -455,18 +473,38 @@ __global__ __launch_bounds__(256 * GROUPS, 2) void prompt_bwd_kv_kernel(const Bw
     }
     if (group == 1) return;
   }
-  if (j0 + i >= nk) return;
-  char* dk = a.dK.p + (int64_t)(sk.first + mine) * a.dK.row + (int64_t)hk * a.dK.head + h * 32;
-  char* dv = a.dV.p + (int64_t)(sk.first + mine) * a.dV.row + (int64_t)hk * a.dV.head + h * 32;
+  if (!OWN) {
+    if (j0 + i >= nk) return;
+    char* dk = a.dK.p + (int64_t)(sk.first + mine) * a.dK.row + (int64_t)hk * a.dK.head + h * 32;
+    char* dv = a.dV.p + (int64_t)(sk.first + mine) * a.dV.row + (int64_t)hk * a.dV.head + h * 32;
 #pragma unroll
-  for (int d = 0; d < DT; ++d) {
-    float x[16], y[16];
+    for (int d = 0; d < DT; ++d) {
+      float x[16], y[16];
 #pragma unroll
-    for (int r = 0; r < 16; ++r) { x[r] = ok[d][r] * a.scale; y[r] = ov[d][r]; }
-    *reinterpret_cast<bf16x8*>(dk + d * 64) = pack8(x);
-    *reinterpret_cast<bf16x8*>(dk + d * 64 + 16) = pack8(x + 8);
-    *reinterpret_cast<bf16x8*>(dv + d * 64) = pack8(y);
-    *reinterpret_cast<bf16x8*>(dv + d * 64 + 16) = pack8(y + 8);
+      for (int r = 0; r < 16; ++r) { x[r] = ok[d][r] * a.scale; y[r] = ov[d][r]; }
+      *reinterpret_cast<bf16x8*>(dk + d * 64) = pack8(x);
+      *reinterpret_cast<bf16x8*>(dk + d * 64 + 16) = pack8(x + 8);
+      *reinterpret_cast<bf16x8*>(dv + d * 64) = pack8(y);
+      *reinterpret_cast<bf16x8*>(dv + d * 64 + 16) = pack8(y + 8);
+    }
+    return;
+  }
+  if (j0 >= nk) return;
+#pragma unroll
+  for (int n = 0; n < 2; ++n) {
+    const f32x16* sum = n == 0 ? ok : ov;
+    const AttnRows& to = n == 0 ? a.dK : a.dV;
+    const float f = n == 0 ? a.scale : 1.f;
+    wave_lds_fence();
+#pragma unroll
+    for (int d = 0; d < DT; ++d) {
+      float x[16];
+#pragma unroll
+      for (int r = 0; r < 16; ++r) x[r] = sum[d][r] * f;
+      put_dims<DH>(own_tile, i, 4 * d + 2 * h, pack8(x), pack8(x + 8));
+    }
+    wave_lds_fence();
+    store_rows<DH>(own_tile, to.p + (sk.first + j0) * to.row + (int64_t)hk * to.head, to.row, nk - j0, lane);
   }
 }
 
