@@ -4,7 +4,6 @@ nothing is computed here or by torch.  Q, K, V and their kin may be views whose 
 fused projection, say) as long as the head dimension is dense and rows start at multiples of 16 bytes."""
 from __future__ import annotations
 
-import contextlib
 import ctypes
 from typing import NamedTuple, Optional
 
@@ -98,128 +97,137 @@ def alloc_decode_workspace(shape: CacheShape, H: int, device="cuda") -> torch.Te
 
 
 _BF16, _F32, _I32, _U8 = torch.bfloat16, torch.float32, torch.int32, torch.uint8
+_byref = ctypes.byref
+_strides2, _strides4, _strides8 = (ctypes.c_int64 * 4), (ctypes.c_int64 * 8), (ctypes.c_int64 * 16)
 
 
-class _Args:
-    """Pointers of a call's tensors, which must all be on the GPU of the first, and the strides of those that
-    may be views (None where all of them are dense)."""
-
-    def __init__(self, first):
-        if not isinstance(first, torch.Tensor) or not first.is_cuda:
-            raise ValueError("need tensors on a GPU")
-        self.device, self.at, self.dense, self.keep = first.device, [], True, None
-
-    def plain(self, t, dtype, numel, name):
-        if t is None:
-            return None
-        if t.device != self.device:
-            raise ValueError(f"{name}: on {t.device}, the other tensors are on {self.device}")
-        return spt._ptr(t, dtype, numel, name)
-
-    def rows(self, t, shape, name):
-        if t.dtype is not _BF16 or tuple(t.shape) != shape or t.device != self.device or (t.stride(2) != 1 and shape[2] != 1):
-            raise ValueError(f"{name}: need a tensor of {_BF16} {shape} on {self.device} with a dense last axis, "
-                             f"got {t.dtype} {tuple(t.shape)} on {t.device}, strides {tuple(t.stride())}")
-        if t.is_contiguous():
-            self.at += (shape[1] * shape[2], shape[2])
-        else:
-            self.dense = False
-            self.at += (t.stride(0), t.stride(1))
-        return t.data_ptr()
-
-    def strides(self):
-        if self.dense:
-            return None
-        self.keep = (ctypes.c_int64 * len(self.at))(*self.at)
-        return ctypes.cast(self.keep, ctypes.c_void_p)
-
-    def here(self):
-        """The calls launch on the current device: make it the tensors'."""
-        if self.device.index == torch._C._cuda_getDevice():
-            return contextlib.nullcontext()
-        return torch.cuda.device(self.device)
+def _gpu(t, name: str) -> int:
+    """The GPU of a call's first tensor, which all others must be on."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError(f"{name}: need a tensor on a GPU")
+    return t.get_device()
 
 
-def _run(a: _Args, name: str, *args):
-    with a.here():
-        spt._check(getattr(lib(), name)(*args, spt._stream()), name)
+def _dense(t, dtype, numel: int, dev: int, name: str):
+    """Pointer of a dense tensor, or None."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.numel() != numel or not t.is_contiguous() or t.get_device() != dev:
+        raise ValueError(f"{name}: need a contiguous tensor of {dtype} with {numel} elements on cuda:{dev}, "
+                         f"got {t.dtype} {tuple(t.shape)} on {t.device}")
+    return t.data_ptr()
+
+
+def _rows(t, shape, dev: int, name: str):
+    """Pointer of rows [T, heads, dh], which may lie apart."""
+    if t.dtype is not _BF16 or t.shape != shape or t.get_device() != dev or t.stride(2) != 1:
+        raise ValueError(f"{name}: need a tensor of {_BF16} {shape} on cuda:{dev} with a dense last axis, "
+                         f"got {t.dtype} {tuple(t.shape)} on {t.device}, strides {tuple(t.stride())}")
+    return t.data_ptr()
+
+
+def _strides(kind, *tensors):
+    """Row and head strides of tensors, or None where all are dense."""
+    for t in tensors:
+        if not t.is_contiguous():
+            return kind(*(n for t in tensors for n in ((t.stride(0), t.stride(1)) if not t.is_contiguous() else
+                                                       (t.shape[1] * t.shape[2], t.shape[2]))))
+    return None
+
+
+def _call(dev: int, name: str, *args):
+    """Calls launch on the current device and its current stream: make it the tensors' device."""
+    f = _functions.get(name) or _functions.setdefault(name, getattr(lib(), name))
+    if dev == torch._C._cuda_getDevice():
+        rc = f(*args, torch._C._cuda_getCurrentRawStream(dev))
+    else:
+        with torch.cuda.device(dev):
+            rc = f(*args, torch._C._cuda_getCurrentRawStream(dev))
+    if rc != 0:
+        raise spt.SptError(rc, name)
+
+
+_functions: dict = {}
 
 
 def prompt_fwd(shape: AttnShape, Q, K, V, cu_q, cu_k, Y=None, lse=None, save_for_backward=True):
     """Y[Tq,H,dh] bf16 and (optionally) lse[H,Tq] fp32 of Q[Tq,H,dh], K, V[Tk,Hk,dh] and the first rows cu_q, cu_k
     [B+1] int32 of the sequences.  Rows behind the last sequence stay as they are."""
-    s, a = shape, _Args(Q)
-    q, k = (s.Tq, s.H, s.dh), (s.Tk, s.Hk, s.dh)
-    Y = torch.empty(q, dtype=_BF16, device=a.device) if Y is None else Y
+    s, dev = shape, _gpu(Q, "Q")
+    B, H, Tq = s.B, s.H, s.Tq
+    q, k = (Tq, H, s.dh), (s.Tk, s.Hk, s.dh)
+    if Y is None:
+        Y = torch.empty(q, dtype=_BF16, device=Q.device)
     if lse is None and save_for_backward:
-        lse = torch.empty((s.H, s.Tq), dtype=_F32, device=a.device)
-    ptrs = [a.rows(Q, q, "Q"), a.rows(K, k, "K"), a.rows(V, k, "V")]
-    y = a.rows(Y, q, "Y")
-    _run(a, "spt_attn_prompt_fwd", ctypes.byref(s), *ptrs, a.strides(), a.plain(cu_q, _I32, s.B + 1, "cu_q"),
-         a.plain(cu_k, _I32, s.B + 1, "cu_k"), y, a.plain(lse, _F32, s.H * s.Tq, "lse"))
+        lse = torch.empty((H, Tq), dtype=_F32, device=Q.device)
+    _call(dev, "spt_attn_prompt_fwd", _byref(s), _rows(Q, q, dev, "Q"), _rows(K, k, dev, "K"), _rows(V, k, dev, "V"),
+          _strides(_strides4, Q, K, V, Y), _dense(cu_q, _I32, B + 1, dev, "cu_q"), _dense(cu_k, _I32, B + 1, dev, "cu_k"),
+          _rows(Y, q, dev, "Y"), _dense(lse, _F32, H * Tq, dev, "lse"))
     return Y, lse
 
 
 def prompt_bwd(shape: AttnShape, Q, K, V, Y, dY, lse, cu_q, cu_k, ws=None, dQ=None, dK=None, dV=None):
     """dQ[Tq,H,dh], dK, dV[Tk,Hk,dh] bf16 from dY[Tq,H,dh] and the forward's Y and lse."""
-    s, a = shape, _Args(Q)
-    q, k = (s.Tq, s.H, s.dh), (s.Tk, s.Hk, s.dh)
-    dQ, dK, dV = (torch.empty(n, dtype=_BF16, device=a.device) if t is None else t for t, n in ((dQ, q), (dK, k), (dV, k)))
-    ws = alloc_prompt_workspace(s, a.device) if ws is None else ws
-    ins = [a.rows(t, n, name) for t, n, name in ((Q, q, "Q"), (K, k, "K"), (V, k, "V"), (Y, q, "Y"), (dY, q, "dY"))]
-    outs = [a.rows(t, n, name) for t, n, name in ((dQ, q, "dQ"), (dK, k, "dK"), (dV, k, "dV"))]
-    _run(a, "spt_attn_prompt_bwd", ctypes.byref(s), *ins, a.plain(lse, _F32, s.H * s.Tq, "lse"), a.strides(),
-         a.plain(cu_q, _I32, s.B + 1, "cu_q"), a.plain(cu_k, _I32, s.B + 1, "cu_k"), *outs,
-         a.plain(ws, _U8, ws.numel(), "ws"), ws.numel())
+    s, dev = shape, _gpu(Q, "Q")
+    B, H, Tq = s.B, s.H, s.Tq
+    q, k = (Tq, H, s.dh), (s.Tk, s.Hk, s.dh)
+    dQ, dK, dV = (torch.empty(n, dtype=_BF16, device=Q.device) if t is None else t for t, n in ((dQ, q), (dK, k), (dV, k)))
+    if ws is None:
+        ws = alloc_prompt_workspace(s, Q.device)
+    _call(dev, "spt_attn_prompt_bwd", _byref(s), _rows(Q, q, dev, "Q"), _rows(K, k, dev, "K"), _rows(V, k, dev, "V"), _rows(Y, q, dev, "Y"),
+          _rows(dY, q, dev, "dY"), _dense(lse, _F32, H * Tq, dev, "lse"), _strides(_strides8, Q, K, V, Y, dY, dQ, dK, dV),
+          _dense(cu_q, _I32, B + 1, dev, "cu_q"), _dense(cu_k, _I32, B + 1, dev, "cu_k"), _rows(dQ, q, dev, "dQ"), _rows(dK, k, dev, "dK"),
+          _rows(dV, k, dev, "dV"), _dense(ws, _U8, ws.numel(), dev, "ws"), ws.numel())
     return dQ, dK, dV
 
 
-def _cache_ptrs(a: _Args, s: CacheShape, cache):
+def _pool(s: CacheShape, cache, dev: int):
     K, V, ks, vs = cache
-    dtype, rows = (_BF16 if s.format == CACHE_BF16 else _U8), s.pages * s.Hk * s.page
-    if dtype is _U8 and K.dtype is torch.float8_e4m3fn:
+    bf, rows = s.format == CACHE_BF16, s.pages * s.Hk * s.page
+    if not bf and K.dtype is torch.float8_e4m3fn:
         K, V = K.view(_U8), V.view(_U8)
-    return [a.plain(K, dtype, rows * s.dh, "cache.K"), a.plain(V, dtype, rows * s.dh, "cache.V"),
-            a.plain(ks, _U8, rows, "cache.ks"), a.plain(vs, _U8, rows, "cache.vs")]
+    dtype, n = _BF16 if bf else _U8, rows * s.dh
+    return (_dense(K, dtype, n, dev, "cache.K"), _dense(V, dtype, n, dev, "cache.V"), _dense(ks, _U8, rows, dev, "cache.ks"),
+            _dense(vs, _U8, rows, dev, "cache.vs"))
 
 
-def _seq_ptrs(a: _Args, s: CacheShape, table, start, cu):
-    return [a.plain(table, _I32, s.B * s.max_pages, "table"), a.plain(start, _I32, s.B, "start"), a.plain(cu, _I32, s.B + 1, "cu")]
+def _move_rows(name: str, s: CacheShape, K, V, cache, table, start, cu, dev: int):
+    n, B = (K.shape[0], s.Hk, s.dh), s.B
+    _call(dev, name, _byref(s), n[0], _rows(K, n, dev, "K"), _rows(V, n, dev, "V"), _strides(_strides2, K, V),
+          _dense(table, _I32, B * s.max_pages, dev, "table"), _dense(start, _I32, B, dev, "start"), _dense(cu, _I32, B + 1, dev, "cu"),
+          *_pool(s, cache, dev))
 
 
 def cache_write(shape: CacheShape, K, V, cache, table, start, cu):
     """Rows cu[b] .. cu[b+1]-1 of K, V [T,Hk,dh] bf16 become tokens start[b], start[b] + 1, ... of sequence b, whose
     pages table[b] names."""
-    s, a = shape, _Args(K)
-    n = (K.shape[0], s.Hk, s.dh)
-    kv = [a.rows(K, n, "K"), a.rows(V, n, "V")]
-    _run(a, "spt_cache_write", ctypes.byref(s), n[0], *kv, a.strides(), *_seq_ptrs(a, s, table, start, cu), *_cache_ptrs(a, s, cache))
+    _move_rows("spt_cache_write", shape, K, V, cache, table, start, cu, _gpu(K, "K"))
     return cache
 
 
 def cache_read(shape: CacheShape, cache, table, start, cu, T=None, K=None, V=None):
     """K, V [T,Hk,dh] bf16: what the cache holds for tokens start[b], start[b] + 1, ... of sequence b, in rows
     cu[b] .. cu[b+1]-1.  Give T, or K and V."""
-    s, a = shape, _Args(cache[0])
+    dev = _gpu(cache[0], "cache.K")
     if K is None or V is None:
-        if T is None and K is None and V is None:
+        T = next((t.shape[0] for t in (K, V) if t is not None), T)
+        if T is None:
             raise ValueError("cache_read: need T, or K and V")
-        T = T if T is not None else (V if K is None else K).shape[0]
-    n = (T if T is not None else K.shape[0], s.Hk, s.dh)
-    K, V = (torch.empty(n, dtype=_BF16, device=a.device) if t is None else t for t in (K, V))
-    kv = [a.rows(K, n, "K"), a.rows(V, n, "V")]
-    _run(a, "spt_cache_read", ctypes.byref(s), n[0], *kv, a.strides(), *_seq_ptrs(a, s, table, start, cu), *_cache_ptrs(a, s, cache))
+        K, V = (torch.empty((T, shape.Hk, shape.dh), dtype=_BF16, device=cache[0].device) if t is None else t for t in (K, V))
+    _move_rows("spt_cache_read", shape, K, V, cache, table, start, cu, dev)
     return K, V
 
 
 def decode(shape: CacheShape, Q, cache, table, lens, scale=None, ws=None, Y=None):
     """Y[B,H,dh] bf16: attention of one query for each sequence, Q[B,H,dh], over the first lens[b] tokens of its pages."""
-    s, a = shape, _Args(Q)
-    n = (s.B, Q.shape[1], s.dh)
-    Y = torch.empty(n, dtype=_BF16, device=a.device) if Y is None else Y
-    ws = alloc_decode_workspace(s, n[1], a.device) if ws is None else ws
-    q, y = a.rows(Q, n, "Q"), a.rows(Y, n, "Y")
-    _run(a, "spt_attn_decode", ctypes.byref(s), n[1], s.dh ** -0.5 if scale is None else scale, q, a.strides(),
-         *_cache_ptrs(a, s, cache), a.plain(table, _I32, s.B * s.max_pages, "table"), a.plain(lens, _I32, s.B, "lens"), y,
-         a.plain(ws, _U8, ws.numel(), "ws"), ws.numel())
+    s, dev = shape, _gpu(Q, "Q")
+    B, H, dh = s.B, Q.shape[1], s.dh
+    n = (B, H, dh)
+    if Y is None:
+        Y = torch.empty(n, dtype=_BF16, device=Q.device)
+    if ws is None:
+        ws = alloc_decode_workspace(s, H, Q.device)
+    _call(dev, "spt_attn_decode", _byref(s), H, dh ** -0.5 if scale is None else scale, _rows(Q, n, dev, "Q"), _strides(_strides2, Q, Y),
+          *_pool(s, cache, dev), _dense(table, _I32, B * s.max_pages, dev, "table"), _dense(lens, _I32, B, dev, "lens"),
+          _rows(Y, n, dev, "Y"), _dense(ws, _U8, ws.numel(), dev, "ws"), ws.numel())
     return Y

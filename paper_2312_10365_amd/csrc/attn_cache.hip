@@ -538,8 +538,8 @@ template <int DH, bool E4M3>
 hipError_t launch_decode(const DecodeArgs& a, hipStream_t st) {
   typedef DecodeTile<DH, E4M3> T;
   constexpr int join = kDecodeWaves * 16 * (2 + DH + 4) * 4, smem = kDecodeWaves * T::RING > join ? kDecodeWaves * T::RING : join;
-  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(decode_kernel<DH, E4M3>), hipFuncAttributeMaxDynamicSharedMemorySize, smem);
-  if (e != hipSuccess) return e;
+  static std::atomic<uint64_t> done{0};
+  if (const hipError_t e = allow_smem(reinterpret_cast<const void*>(decode_kernel<DH, E4M3>), smem, done); e != hipSuccess) return e;
   {
     ScopedKernelTimer timer(kSlotAttnDecode, st);
     hipLaunchKernelGGL((decode_kernel<DH, E4M3>), dim3(a.workgroups), dim3(64 * kDecodeWaves), smem, st, a);

@@ -4,6 +4,8 @@
 #include <limits.h>
 #include <math.h>
 
+#include <atomic>
+
 #include "../../include/spt_attn.h"
 #include "ffn_common.hpp"
 #include "profile.hpp"
@@ -33,6 +35,17 @@ inline int attn_rows(AttnRows* r, const void* p, const int64_t* strides, int64_t
   }
   *r = AttnRows{const_cast<char*>(static_cast<const char*>(p)), row * 2, head * 2};
   return SPT_OK;
+}
+
+// Lets a kernel use `smem` bytes of LDS: asked for once on each GPU (a call of the runtime costs a launch a tenth of its time).
+inline hipError_t allow_smem(const void* kernel, int smem, std::atomic<uint64_t>& done) {
+  int dev = 0;
+  if (const hipError_t e = hipGetDevice(&dev); e != hipSuccess) return e;
+  const uint64_t bit = 1ull << (dev & 63);
+  if (dev < 64 && (done.load(std::memory_order_relaxed) & bit)) return hipSuccess;
+  const hipError_t e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (e == hipSuccess) done.fetch_or(bit, std::memory_order_relaxed);
+  return e;
 }
 
 int check_attn(const spt_attn_shape_t* s);   // attn_prompt.hip

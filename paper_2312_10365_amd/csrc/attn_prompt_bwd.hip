@@ -511,8 +511,8 @@ __global__ __launch_bounds__(256 * GROUPS, 2) void prompt_bwd_kv_kernel(const Bw
 template <int DH, int GROUPS>
 hipError_t launch_kv(const BwdArgs& a, int grid, hipStream_t st) {
   constexpr int smem = KvSizes<DH, GROUPS>::SMEM;
-  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(prompt_bwd_kv_kernel<DH, GROUPS>), hipFuncAttributeMaxDynamicSharedMemorySize, smem);
-  if (e != hipSuccess) return e;
+  static std::atomic<uint64_t> done{0};
+  if (const hipError_t e = allow_smem(reinterpret_cast<const void*>(prompt_bwd_kv_kernel<DH, GROUPS>), smem, done); e != hipSuccess) return e;
   hipLaunchKernelGGL((prompt_bwd_kv_kernel<DH, GROUPS>), dim3(grid), dim3(256 * GROUPS), smem, st, a);
   return hipGetLastError();
 }
