@@ -153,17 +153,18 @@ __global__ __launch_bounds__(256) void cache_read_kernel(const RowArgs a) {
 
 // ------------------------------------------------------------------------------------------
 // Decoding.  The cache is read once; everything else is small.  An item is a key head of a sequence with up to 16 of the
-// query heads that read it (the columns of a 16 x 16 x 32 product), a unit 32 tokens of an item.  The units of all items stand in one line, and
-// every workgroup takes an equal stretch of it, whatever the lengths: an item that lies within one workgroup's stretch is
-// finished there, the others leave a partial result (maximum, sum, unnormalised output) per workgroup, which a second launch
-// joins in the order of the cache.  At most the first and the last item of a stretch are partial: two slots a workgroup.
-// In a workgroup the four wavefronts take turns at the units of an item, each with a ring of two units in LDS of its own,
-// filled by asynchronous copies: no barrier but at an item's end.  Scores are formed transposed (rows: tokens), so that
+// query heads that read it (the columns of a 16 x 16 x 32 product), a unit 32 tokens of an item.  The units of all items stand in one
+// line, and every wavefront takes an equal stretch of it, whatever the lengths: an item that lies within one stretch is
+// finished there, the others leave a partial result (maximum, sum, unnormalised output) per stretch, which a second launch
+// joins in the order of the cache.  At most the first and the last item of a stretch are partial: two slots a stretch.
+// Wavefronts do not wait for one another.  Each has a ring of two units in LDS of its own, filled by asynchronous copies that run
+// ahead over the ends of items (with a wavefront per unit in turn, and a workgroup's four joined at every item's end, 48 sequences of 100 to 8000
+// tokens, 8 key heads, went at 4.0 TB/s, eight of one length at 5.0).  Scores are formed transposed (rows: tokens), so that
 // a lane holds the weights of one query as the second product wants them; a weight goes into it as the sum of two bf16 (the
-// matrix cores have nothing else to do), so the weights are exact to 2^-17.  8-bit codes become bf16 in registers, exactly; the rows' exponents are
-// applied to the scores and to the weights.
+// matrix cores have nothing else to do), so the weights are exact to 2^-17.  8-bit codes become bf16 in registers, exactly; the
+// rows' exponents are applied to the scores and to the weights.
 
-constexpr int kUnit = 32, kDecodeWaves = 4;
+constexpr int kUnit = 32, kDecodeWaves = 4, kLeastUnits = 2;   // (a stretch has two units at least, so that there is something to run ahead to)
 
 struct DecodeArgs {
   CacheArgs c;
@@ -175,305 +176,356 @@ struct DecodeArgs {
   float cs;                       // scale log2 e
 };
 
-__device__ __forceinline__ int seq_units(const DecodeArgs& a, int b) {
-  const int cap = a.c.max_pages << a.c.page_shift;
-  return (min(max(a.lens[b], 0), cap) + kUnit - 1) / kUnit;
-}
+__device__ __forceinline__ int units_of(int len) { return (len + kUnit - 1) / kUnit; }
+__device__ __forceinline__ int seq_len(const DecodeArgs& a, int len) { return min(max(len, 0), a.c.max_pages << a.c.page_shift); }
+__device__ __forceinline__ int seq_units(const DecodeArgs& a, int b) { return units_of(seq_len(a, a.lens[b])); }
 
 struct Line { int total, share; };
-// Units of all sequences, and a workgroup's part of them.
+// Units of all sequences, and a wavefront's part of them.
 __device__ __forceinline__ Line unit_line(const DecodeArgs& a) {
   int n = 0;
   for (int b = threadIdx.x & 63; b < a.c.B; b += 64) n += seq_units(a, b);
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) n += __shfl_xor(n, o);
-  n = __builtin_amdgcn_readfirstlane(n) * a.c.Hk * a.sets;
-  return {n, max(1, (n + a.workgroups - 1) / a.workgroups)};
+  n = wave_total(n) * a.c.Hk * a.sets;
+  const int waves = a.workgroups * kDecodeWaves;
+  return {n, max(kLeastUnits, (n + waves - 1) / waves)};
 }
 // First unit of sequence b's items
 __device__ __forceinline__ int units_before(const DecodeArgs& a, int b) {
   int n = 0;
   for (int x = threadIdx.x & 63; x < b; x += 64) n += seq_units(a, x);
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) n += __shfl_xor(n, o);
-  return __builtin_amdgcn_readfirstlane(n) * a.c.Hk * a.sets;
+  return wave_total(n) * a.c.Hk * a.sets;
 }
 
-template <int DH, bool E4M3>
+// QCOPIES: the copies of 1 KB that an item's queries take, one or as many as sixteen heads need: LDS that other wavefronts could use.
+template <int DH, bool E4M3, int QC>
 struct DecodeTile {
   static constexpr int RB = E4M3 ? DH : DH * 2;            // bytes of a row
   static constexpr int BYTES = kUnit * RB;                 // of a unit's K or V
   static constexpr int COPIES = BYTES / 1024;
-  static constexpr int STAGE = 2 * BYTES + (E4M3 ? 256 : 0);
+  static constexpr int QCOPIES = QC, QUERIES = QC * 1024;  // of an item, with its first unit
+  static constexpr int STAGE = 2 * BYTES + QUERIES + (E4M3 ? 256 : 0);
   static constexpr int LOADS = 2 * COPIES + (E4M3 ? 1 : 0);
-  static constexpr int RING = 2 * STAGE;
+  static constexpr int RING = 2 * STAGE, SMEM = kDecodeWaves * RING, PER_CU = 160 * 1024 / SMEM;
+  static_assert(PER_CU >= 1, "a CU's LDS");
+};
+constexpr int kQueryRows[2] = {8, 4};                      // heads whose queries fit into one copy: dh 64, 128
+
+// A unit: its sequence, its item and place in it, its pages.
+struct Unit {
+  int b, item, t, units, len;     // units, len: of the sequence
+  int page[2];                    // of its two halves
 };
 
-template <int DH, bool E4M3>
-__global__ __launch_bounds__(64 * kDecodeWaves) void decode_kernel(const DecodeArgs a) {
-  typedef DecodeTile<DH, E4M3> T;
+template <int DH, bool E4M3, int QC>
+__global__ __launch_bounds__(64 * kDecodeWaves, 2) void decode_kernel(const DecodeArgs a) {
+  typedef DecodeTile<DH, E4M3, QC> T;
   constexpr int RB = T::RB, KS = DH / 32, DT = DH / 16;
   extern __shared__ __align__(256) char smem[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int q = lane & 15, c = lane >> 4;
+  const int q = lane & 15, c = lane >> 4, items = a.c.Hk * a.sets, qrow = min(q, QC * (512 / DH) - 1);
   char* ring = smem + wave * T::RING;
 
   const Line line = unit_line(a);
-  int u = blockIdx.x * line.share;
-  const int uend = min(line.total, u + line.share);
-  if (u >= uend) return;
-  // the sequence of unit u
-  int b = 0, rem = u;
-  {
-    const int per = a.c.Hk * a.sets;
-    int before = 0;
-    for (int b0 = 0; b0 < a.c.B; b0 += 64) {
-      int incl = b0 + lane < a.c.B ? seq_units(a, b0 + lane) * per : 0;
+  const int stretch = wave * a.workgroups + blockIdx.x;    // (few stretches: one on a CU)
+  if (stretch > line.total / line.share) return;
+  int left = min(line.total - stretch * line.share, line.share);
+  if (left <= 0) return;
+
+  auto pages_of = [&](Unit& x) {
 #pragma unroll
-      for (int o = 1; o < 64; o <<= 1) {
-        const int up = __shfl_up(incl, o);
-        if (lane >= o) incl += up;
-      }
-      const int total = __builtin_amdgcn_readlane(incl, 63);
+    for (int half = 0; half < 2; ++half)
+      x.page[half] = uniform_load(a.c.table + (int64_t)x.b * a.c.max_pages + (min(x.t * kUnit + 16 * half, x.len - 1) >> a.c.page_shift));
+  };
+  auto sequence = [&](Unit& x) {
+    x.len = seq_len(a, uniform_load(a.lens + x.b));
+    x.units = units_of(x.len);
+  };
+  Unit ahead;                                              // the next unit to be asked for
+  {
+    const int u = stretch * line.share;
+    int before = 0, rem = 0;
+    ahead.b = 0;
+    for (int b0 = 0; b0 < a.c.B; b0 += 64) {
+      const int incl = wave_prefix(b0 + lane < a.c.B ? seq_units(a, b0 + lane) : 0) * items, total = __builtin_amdgcn_readlane(incl, 63);
       if (u - before < total) {
         const int src = __builtin_ctzll(__ballot(incl > u - before));
-        b = b0 + src;
+        ahead.b = b0 + src;
         rem = u - before - (src > 0 ? __builtin_amdgcn_readlane(incl, src - 1) : 0);
         break;
       }
       before += total;
     }
+    sequence(ahead);
+    ahead.item = rem / ahead.units;
+    ahead.t = rem - ahead.item * ahead.units;
+    pages_of(ahead);
   }
-
-  for (bool first_item = true; u < uend; first_item = false) {
-    const int cap = a.c.max_pages << a.c.page_shift;
-    const int len = min(max(uniform_load(a.lens + b), 0), cap), units = (len + kUnit - 1) / kUnit;
-    if (units == 0) { ++b; continue; }
-    const int item = rem / units, t0 = rem - item * units, t1 = min(units, t0 + uend - u);
-    const int hk = item / a.sets, head0 = hk * a.G + (item - hk * a.sets) * 16, heads = min(16, (hk + 1) * a.G - head0);
-
-    bf16x8 qf[KS];
-    const char* qrow = a.Q.p + b * a.Q.row + (int64_t)(head0 + min(q, heads - 1)) * a.Q.head;
-#pragma unroll
-    for (int s = 0; s < KS; ++s) qf[s] = *reinterpret_cast<const bf16x8*>(qrow + s * 64 + c * 16);
-
-    const int32_t* table = a.c.table + (int64_t)b * a.c.max_pages;
-    // copies of unit t into a stage; returns which of its 32 tokens are there
-    auto fetch = [&](int t, int stage) -> uint32_t {
-      const uint32_t at = lds_addr(ring + stage * T::STAGE);
-      uint32_t there = 0;
-      int64_t row[2];
-#pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        const int pos = t * kUnit + 16 * half;
-        int page = pos < len ? uniform_load(table + (pos >> a.c.page_shift)) : -1;
-        if (page >= 0 && page < a.c.pages) there |= (len - pos >= 16 ? 0xFFFFu : (1u << (len - pos)) - 1u) << (16 * half);
-        else page = 0;
-        row[half] = ((((int64_t)page * a.c.Hk) + hk) << a.c.page_shift) + (pos & ((1 << a.c.page_shift) - 1));
+  auto advance = [&](Unit& x) {                            // (there is one more unit)
+    if (++x.t == x.units) {
+      x.t = 0;
+      if (++x.item == items) {
+        x.item = 0;
+        do {
+          ++x.b;
+          sequence(x);
+        } while (x.units == 0);
       }
+    }
+    pages_of(x);
+  };
+  auto head0_of = [&](const Unit& x) { return x.item / a.sets * a.G + x.item % a.sets * 16; };
+  auto heads_of = [&](const Unit& x) { return min(16, a.G - x.item % a.sets * 16); };
+
+  // copies of a unit into a stage (with its item's queries where these are new); returns which of its 32 tokens are there
+  auto fetch = [&](const Unit& x, bool queries, int stage) -> uint32_t {
+    const uint32_t at = lds_addr(ring + stage * T::STAGE);
+    const int hk = x.item / a.sets;
+    uint32_t there = 0;
+    int64_t row[2];
 #pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      const int pos = x.t * kUnit + 16 * half;
+      const bool ok = pos < x.len && x.page[half] >= 0 && x.page[half] < a.c.pages;
+      if (ok) there |= (x.len - pos >= 16 ? 0xFFFFu : (1u << (x.len - pos)) - 1u) << (16 * half);
+      row[half] = ((((int64_t)(ok ? x.page[half] : 0) * a.c.Hk) + hk) << a.c.page_shift) + (pos & ((1 << a.c.page_shift) - 1));
+    }
+#pragma unroll
+    for (int n = 0; n < T::COPIES; ++n) {
+      const int r = n * (1024 / RB) + lane / (RB / 16);    // row of the unit; those of a copy lie in one half
+      const int half = n * (1024 / RB) / 16;
+      const uint32_t off = (uint32_t)(r - 16 * half) * RB + (((uint32_t)lane % (RB / 16)) ^ chunk_swizzle<RB>(r)) * 16;
+      dma16_at(a.c.Kc + row[half] * RB, off, at + n * 1024);
+      dma16_at(a.c.Vc + row[half] * RB, off, at + T::BYTES + n * 1024);
+    }
+    if (E4M3) {                                            // lanes 0-7: exponents of the keys, 8-15: of the values
+      const int half = (lane >> 2) & 1;
+      dma4(((lane & 8) ? a.c.vs : a.c.ks) + row[half] + 4 * (lane & 3), at + 2 * T::BYTES + T::QUERIES);
+    }
+    if (queries) {
+      const char* base = a.Q.p + x.b * a.Q.row + (int64_t)head0_of(x) * a.Q.head;
+      const int heads = heads_of(x);
+#pragma unroll
+      for (int n = 0; n < T::QCOPIES; ++n) {
+        const int r = n * (512 / DH) + lane / (DH / 8);    // (rows past the heads: the last one again)
+        dma16_at(base, (uint32_t)min(r, heads - 1) * (uint32_t)a.Q.head + (((uint32_t)lane % (DH / 8)) ^ row_swizzle<DH>(r)) * 16,
+                 at + 2 * T::BYTES + n * 1024);
+      }
+    }
+    return there;
+  };
+
+  bf16x8 qf[KS];
+  f32x4 o[DT];
+  float m, neg_m, l;
+  Unit now = ahead, next = ahead;
+  bool fresh = true, next_fresh = false, first_item = true;   // whether a unit's queries are new
+  int item_units = 0;                                      // units of the present item so far
+  uint32_t there = fetch(now, true, 0), next_there = 0;
+  --left;
+  if (left > 0) {
+    advance(ahead);
+    next = ahead;
+    next_fresh = next.t == 0;
+    next_there = fetch(next, next_fresh, 1);
+    if (left > 1) advance(ahead);
+  }
+  for (int stage = 0;; stage ^= 1) {
+    if (left <= 0) wait_vmcnt<0>();
+    else if (next_fresh) wait_vmcnt<T::LOADS + T::QCOPIES>();
+    else wait_vmcnt<T::LOADS>();
+    wave_lds_fence();
+    char* kt = ring + stage * T::STAGE;
+    char* vt = kt + T::BYTES;
+    if (fresh) {
+#pragma unroll
+      for (int s = 0; s < KS; ++s)
+        qf[s] = *reinterpret_cast<const bf16x8*>(kt + 2 * T::BYTES + qrow * (DH * 2) + ((uint32_t)(4 * s + c) ^ row_swizzle<DH>(qrow)) * 16);
+#pragma unroll
+      for (int d = 0; d < DT; ++d) o[d] = f32x4{0.f, 0.f, 0.f, 0.f};
+      m = -INFINITY; neg_m = 0.f; l = 0.f;
+      item_units = 0;
+    }
+    ++item_units;
+    if (there != 0xFFFFFFFFu) {                            // 0 times what lies behind the last token may be NaN
       for (int n = 0; n < T::COPIES; ++n) {
-        const int r = n * (1024 / RB) + lane / (RB / 16);    // row of the unit; 16 n' .. of one half
-        const int half = n * (1024 / RB) / 16;
-        const uint32_t off = (uint32_t)(r - 16 * half) * RB + (((uint32_t)lane % (RB / 16)) ^ chunk_swizzle<RB>(r)) * 16;
-        dma16_at(a.c.Kc + row[half] * RB, off, at + n * 1024);
-        dma16_at(a.c.Vc + row[half] * RB, off, at + T::BYTES + n * 1024);
-      }
-      if (E4M3) {                                            // lanes 0-7: exponents of the keys, 8-15: of the values
-        const int half = (lane >> 2) & 1;
-        dma4(((lane & 8) ? a.c.vs : a.c.ks) + row[half] + 4 * (lane & 3), at + 2 * T::BYTES);
-      }
-      return there;
-    };
-
-    f32x4 o[DT];
-#pragma unroll
-    for (int d = 0; d < DT; ++d) o[d] = f32x4{0.f, 0.f, 0.f, 0.f};
-    float m = -INFINITY, neg_m = 0.f, l = 0.f;
-
-    wait_vmcnt<0>();                                         // (stores of the item before)
-    int t = t0 + wave;
-    uint32_t there = 0, next = 0;
-    if (t < t1) there = fetch(t, 0);
-    for (int stage = 0; t < t1; t += kDecodeWaves, stage ^= 1, there = next) {
-      if (t + kDecodeWaves < t1) {
-        next = fetch(t + kDecodeWaves, stage ^ 1);
-        wait_vmcnt<T::LOADS>();
-      } else {
-        wait_vmcnt<0>();
+        const int r = n * (1024 / RB) + lane / (RB / 16);
+        if (!((there >> r) & 1)) *reinterpret_cast<u32x4*>(vt + n * 1024 + lane * 16) = u32x4{0, 0, 0, 0};
       }
       wave_lds_fence();
-      char* kt = ring + stage * T::STAGE;
-      char* vt = kt + T::BYTES;
-      if (there != 0xFFFFFFFFu) {                            // 0 times what lies behind the last token may be NaN
-        for (int n = 0; n < T::COPIES; ++n) {
-          const int r = n * (1024 / RB) + lane / (RB / 16);
-          if (!((there >> r) & 1)) *reinterpret_cast<u32x4*>(vt + n * 1024 + lane * 16) = u32x4{0, 0, 0, 0};
-        }
-        wave_lds_fence();
-      }
-      f32x4 s[2];
+    }
+    f32x4 s[2];
 #pragma unroll
-      for (int kt2 = 0; kt2 < 2; ++kt2) {
-        s[kt2] = f32x4{0.f, 0.f, 0.f, 0.f};
-        const int r = 16 * kt2 + q;
+    for (int kt2 = 0; kt2 < 2; ++kt2) {
+      s[kt2] = f32x4{0.f, 0.f, 0.f, 0.f};
+      const int r = 16 * kt2 + q;
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-          bf16x8 f;
-          if (E4M3) {
-            const uint32_t piece = 4 * ks + c;
-            const uint2 w = *reinterpret_cast<const uint2*>(kt + r * RB + ((piece >> 1) ^ chunk_swizzle<RB>(r)) * 16 + (piece & 1) * 8);
-            const uint2 lo = uncode4(w.x, 1.f), hi = uncode4(w.y, 1.f);
-            f = as_bf16x8(u32x4{lo.x, lo.y, hi.x, hi.y});
-          } else {
-            f = *reinterpret_cast<const bf16x8*>(kt + r * RB + ((uint32_t)(4 * ks + c) ^ chunk_swizzle<RB>(r)) * 16);
-          }
-          s[kt2] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, qf[ks], s[kt2], 0, 0, 0);
-        }
-      }
-      uint32_t kb[2] = {0, 0}, vb[2] = {0, 0};               // exponents of the lane's tokens 16 kt2 + 4 c + e
-      if (E4M3) {
-        const uint32_t* ex = reinterpret_cast<const uint32_t*>(kt + 2 * T::BYTES);
-        kb[0] = ex[c]; kb[1] = ex[4 + c];
-        vb[0] = ex[8 + c]; vb[1] = ex[12 + c];
-      }
-      float x[8], top = -INFINITY;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        float v = s[e >> 2][e & 3] * a.cs;
-        if (E4M3) v = __builtin_ldexpf(v, (int)((kb[e >> 2] >> (8 * (e & 3))) & 255u) - 127);
-        x[e] = (there >> (16 * (e >> 2) + 4 * c + (e & 3))) & 1 ? v : -INFINITY;
-        top = fmaxf(top, x[e]);
-      }
-      top = fmaxf(top, __shfl_xor(top, 16));
-      top = fmaxf(top, __shfl_xor(top, 32));
-      if (__any(top > m)) {
-        const float mn = fmaxf(m, top), ms = mn == -INFINITY ? 0.f : mn, alpha = __builtin_amdgcn_exp2f(m - ms);
-        m = mn;
-        neg_m = -ms;
-        l *= alpha;
-#pragma unroll
-        for (int d = 0; d < DT; ++d)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) o[d][e] *= alpha;
-      }
-      float w[8], rest[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float p = __builtin_amdgcn_exp2f(x[e] + neg_m);
-        l += p;
-        w[e] = p;
-        if (E4M3) {
-          w[e] = __builtin_ldexpf(p, (int)((vb[e >> 2] >> (8 * (e & 3))) & 255u) - 127);
-          if (!((there >> (16 * (e >> 2) + 4 * c + (e & 3))) & 1)) w[e] = 0.f;
-        }
-      }
-      const bf16x8 hi = pack8(w);
-      const u32x4 hw = __builtin_bit_cast(u32x4, hi);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) rest[e] = w[e] - (e & 1 ? hi_bf16(hw[e >> 1]) : lo_bf16(hw[e >> 1]));
-      const bf16x8 lo = pack8(rest);
-      const int sl = lane & 15;
-#pragma unroll
-      for (int d = 0; d < DT; ++d) {
+      for (int ks = 0; ks < KS; ++ks) {
         bf16x8 f;
         if (E4M3) {
-          const int rr = sl >> 1, r = 4 * c + (rr & 3) + 16 * (rr >> 2);
-          typedef int v2i __attribute__((ext_vector_type(2)));
-          const v2i w8 = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
-              (__attribute__((address_space(3))) v2i*)(uintptr_t)(vt + r * RB + ((uint32_t)d ^ chunk_swizzle<RB>(r)) * 16 + (sl & 1) * 8));
-          const uint2 f0 = uncode4((uint32_t)w8[0], 1.f), f1 = uncode4((uint32_t)w8[1], 1.f);
-          f = as_bf16x8(u32x4{f0.x, f0.y, f1.x, f1.y});
+          const uint32_t piece = 4 * ks + c;
+          const uint2 w = *reinterpret_cast<const uint2*>(kt + r * RB + ((piece >> 1) ^ chunk_swizzle<RB>(r)) * 16 + (piece & 1) * 8);
+          const uint2 lo = uncode4(w.x, 1.f), hi = uncode4(w.y, 1.f);
+          f = as_bf16x8(u32x4{lo.x, lo.y, hi.x, hi.y});
         } else {
-          const int r = 4 * c + (sl >> 2);
-          const uint32_t chunk = 2 * d + ((sl & 3) >> 1);
-          f = tr_read_frag(vt + r * RB + (chunk ^ chunk_swizzle<RB>(r)) * 16 + (sl & 1) * 8,
-                           vt + (r + 16) * RB + (chunk ^ chunk_swizzle<RB>(r + 16)) * 16 + (sl & 1) * 8);
+          f = *reinterpret_cast<const bf16x8*>(kt + r * RB + ((uint32_t)(4 * ks + c) ^ chunk_swizzle<RB>(r)) * 16);
         }
-        o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, hi, o[d], 0, 0, 0);
-        o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, lo, o[d], 0, 0, 0);
+        s[kt2] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, qf[ks], s[kt2], 0, 0, 0);
       }
-      wave_lds_fence();
     }
-    l += __shfl_xor(l, 16);
-    l += __shfl_xor(l, 32);
-
-    // the four wavefronts' results, joined in order
-    __syncthreads();
-    float* ml = reinterpret_cast<float*>(smem);              // [wave][16][2]
-    float* os = ml + kDecodeWaves * 32;                      // [wave][16][DH + 4]
-    constexpr int LD = DH + 4;
-    if (c == 0) { ml[(wave * 16 + q) * 2] = m; ml[(wave * 16 + q) * 2 + 1] = l; }
+    uint32_t kb[2] = {0, 0}, vb[2] = {0, 0};               // exponents of the lane's tokens 16 kt2 + 4 c + e
+    if (E4M3) {
+      const uint32_t* ex = reinterpret_cast<const uint32_t*>(kt + 2 * T::BYTES + T::QUERIES);
+      kb[0] = ex[c]; kb[1] = ex[4 + c];
+      vb[0] = ex[8 + c]; vb[1] = ex[12 + c];
+    }
+    float x[8], top = -INFINITY;
 #pragma unroll
-    for (int d = 0; d < DT; ++d) *reinterpret_cast<f32x4*>(os + (wave * 16 + q) * LD + 16 * d + 4 * c) = o[d];
-    __syncthreads();
-    const bool whole = t0 == 0 && t1 == units;
-    const int slot = 2 * blockIdx.x + (first_item ? 0 : 1);
-    for (int n = threadIdx.x; n < heads * (DH / 4); n += 64 * kDecodeWaves) {
-      const int row = n / (DH / 4), d4 = n % (DH / 4);
-      float M = -INFINITY;
+    for (int e = 0; e < 8; ++e) {
+      float v = s[e >> 2][e & 3] * a.cs;
+      if (E4M3) v = __builtin_ldexpf(v, (int)((kb[e >> 2] >> (8 * (e & 3))) & 255u) - 127);
+      x[e] = (there >> (16 * (e >> 2) + 4 * c + (e & 3))) & 1 ? v : -INFINITY;
+      top = fmaxf(top, x[e]);
+    }
+    top = fmaxf(top, __shfl_xor(top, 16));
+    top = fmaxf(top, __shfl_xor(top, 32));
+    if (__any(top > m)) {
+      const float mn = fmaxf(m, top), ms = mn == -INFINITY ? 0.f : mn, alpha = __builtin_amdgcn_exp2f(m - ms);
+      m = mn;
+      neg_m = -ms;
+      l *= alpha;
 #pragma unroll
-      for (int w2 = 0; w2 < kDecodeWaves; ++w2) M = fmaxf(M, ml[(w2 * 16 + row) * 2]);
-      const float ms = M == -INFINITY ? 0.f : M;
-      f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-      float L = 0.f;
+      for (int d = 0; d < DT; ++d)
 #pragma unroll
-      for (int w2 = 0; w2 < kDecodeWaves; ++w2) {
-        const float f = __builtin_amdgcn_exp2f(ml[(w2 * 16 + row) * 2] - ms);
-        L = fmaf(f, ml[(w2 * 16 + row) * 2 + 1], L);
-        const f32x4 x = *reinterpret_cast<const f32x4*>(os + (w2 * 16 + row) * LD + 4 * d4);
+        for (int e = 0; e < 4; ++e) o[d][e] *= alpha;
+    }
+    float w[8], rest[8];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) sum[e] = fmaf(f, x[e], sum[e]);
+    for (int e = 0; e < 8; ++e) {
+      const float p = __builtin_amdgcn_exp2f(x[e] + neg_m);
+      l += p;
+      w[e] = p;
+      if (E4M3) {
+        w[e] = __builtin_ldexpf(p, (int)((vb[e >> 2] >> (8 * (e & 3))) & 255u) - 127);
+        if (!((there >> (16 * (e >> 2) + 4 * c + (e & 3))) & 1)) w[e] = 0.f;
       }
-      if (whole) {
-        const float inv = L == 0.f ? 0.f : 1.f / L;
-        *reinterpret_cast<uint2*>(a.Y.p + b * a.Y.row + (int64_t)(head0 + row) * a.Y.head + d4 * 8) =
-            make_uint2(pack_bf16x2(sum[0] * inv, sum[1] * inv), pack_bf16x2(sum[2] * inv, sum[3] * inv));
+    }
+    const bf16x8 hi = pack8(w);
+    const u32x4 hw = __builtin_bit_cast(u32x4, hi);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) rest[e] = w[e] - (e & 1 ? hi_bf16(hw[e >> 1]) : lo_bf16(hw[e >> 1]));
+    const bf16x8 lo = pack8(rest);
+    const int sl = lane & 15;
+#pragma unroll
+    for (int d = 0; d < DT; ++d) {
+      bf16x8 f;
+      if (E4M3) {
+        const int rr = sl >> 1, r = 4 * c + (rr & 3) + 16 * (rr >> 2);
+        typedef int v2i __attribute__((ext_vector_type(2)));
+        const v2i w8 = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
+            (__attribute__((address_space(3))) v2i*)(uintptr_t)(vt + r * RB + ((uint32_t)d ^ chunk_swizzle<RB>(r)) * 16 + (sl & 1) * 8));
+        const uint2 f0 = uncode4((uint32_t)w8[0], 1.f), f1 = uncode4((uint32_t)w8[1], 1.f);
+        f = as_bf16x8(u32x4{f0.x, f0.y, f1.x, f1.y});
       } else {
-        const int64_t at = (int64_t)slot * a.rows + row;
-        *reinterpret_cast<f32x4*>(a.part + at * DH + 4 * d4) = sum;
-        if (d4 == 0) { a.stat[at * 2] = M; a.stat[at * 2 + 1] = L; }
+        const int r = 4 * c + (sl >> 2);
+        const uint32_t chunk = 2 * d + ((sl & 3) >> 1);
+        f = tr_read_frag(vt + r * RB + (chunk ^ chunk_swizzle<RB>(r)) * 16 + (sl & 1) * 8,
+                         vt + (r + 16) * RB + (chunk ^ chunk_swizzle<RB>(r + 16)) * 16 + (sl & 1) * 8);
       }
+      o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, hi, o[d], 0, 0, 0);
+      o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, lo, o[d], 0, 0, 0);
     }
-    __syncthreads();
-    u += t1 - t0;
-    rem += t1 - t0;
-    if (rem == units * a.c.Hk * a.sets) { ++b; rem = 0; }
+    // the stage has been read (lgkmcnt 0: no read of it is on its way): the unit after the next one's
+    wave_lds_fence();
+    __builtin_amdgcn_s_waitcnt(0xC07F);
+    const Unit done = now;
+    const bool ends = left <= 0 || next_fresh;
+    now = next;
+    there = next_there;
+    fresh = next_fresh;
+    const bool more = left-- > 0;
+    if (left > 0) {
+      next = ahead;
+      next_fresh = next.t == 0;
+      next_there = fetch(next, next_fresh, stage);
+      if (left > 1) advance(ahead);
+    }
+    if (ends) {                                            // the item's result, or the stretch's part of it
+      float sum = l + __shfl_xor(l, 16);
+      sum += __shfl_xor(sum, 32);
+      const int head0 = head0_of(done);
+      if (q < heads_of(done)) {
+        if (item_units == done.units) {
+          const float inv = sum == 0.f ? 0.f : 1.f / sum;
+          char* y = a.Y.p + done.b * a.Y.row + (int64_t)(head0 + q) * a.Y.head + c * 8;
+#pragma unroll
+          for (int d = 0; d < DT; ++d)
+            *reinterpret_cast<uint2*>(y + d * 32) = make_uint2(pack_bf16x2(o[d][0] * inv, o[d][1] * inv), pack_bf16x2(o[d][2] * inv, o[d][3] * inv));
+        } else {
+          const int64_t row = (int64_t)(2 * stretch + (first_item ? 0 : 1)) * a.rows + q;
+#pragma unroll
+          for (int d = 0; d < DT; ++d) *reinterpret_cast<f32x4*>(a.part + row * DH + 16 * d + 4 * c) = o[d];
+          if (c == 0) {
+            a.stat[row * 2] = m;
+            a.stat[row * 2 + 1] = sum;
+          }
+        }
+      }
+      first_item = false;
+    }
+    if (!more) break;
   }
 }
 
-// One wavefront per query head: the partial results of its item in the order of the cache, or zeros without a key.
+// A workgroup per query head: the partial results of its item in the order of the cache, or zeros without a key.  Eight (dh 128) or
+// sixteen parts of the list side by side, joined in order.
 template <int DH>
 __global__ __launch_bounds__(256) void decode_join_kernel(const DecodeArgs a) {
-  const int lane = threadIdx.x & 63, row = blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (row >= a.c.B * a.H) return;
-  const int b = row / a.H, head = row - b * a.H, hk = head / a.G, g = head - hk * a.G;
-  const int units = seq_units(a, b);
+  constexpr int LANES = DH / 4, PARTS = 256 / LANES;
+  __shared__ f32x4 sums[PARTS][LANES];
+  __shared__ float weight[PARTS], tops[4];
+  const int lane = threadIdx.x & 63, b = blockIdx.x / a.H, head = blockIdx.x - b * a.H, hk = head / a.G, g = head - hk * a.G;
+  const int units = seq_units(a, b), d4 = threadIdx.x % LANES, part = threadIdx.x / LANES;
   char* y = a.Y.p + b * a.Y.row + (int64_t)head * a.Y.head;
-  constexpr int N = DH / 64;
   if (units == 0) {
-#pragma unroll
-    for (int d = 0; d < N; ++d) reinterpret_cast<uint16_t*>(y)[N * lane + d] = 0;
+    if (part == 0) *reinterpret_cast<uint2*>(y + d4 * 8) = make_uint2(0u, 0u);
     return;
   }
   const Line line = unit_line(a);
   const int u0 = units_before(a, b) + (hk * a.sets + g / 16) * units, u1 = u0 + units;
-  const int w0 = u0 / line.share, w1 = (u1 - 1) / line.share;
-  if (w0 == w1) return;                                      // finished where it was read
-  float M = -INFINITY, L = 0.f, sum[N] = {};
-  for (int w = w0; w <= w1; ++w) {
-    const int slot = 2 * w + (w == w0 && w0 * line.share != u0 ? 1 : 0);
-    const int64_t at = (int64_t)slot * a.rows + g % 16;
-    const float m = a.stat[at * 2], l = a.stat[at * 2 + 1], mn = fmaxf(M, m), ms = mn == -INFINITY ? 0.f : mn;
-    const float f = __builtin_amdgcn_exp2f(m - ms), old = __builtin_amdgcn_exp2f(M - ms);
-    M = mn;
-    L = fmaf(L, old, f * l);
+  const int s0 = u0 / line.share, s1 = (u1 - 1) / line.share;
+  if (s0 == s1) return;                                      // finished where it was read
+  auto row_of = [&](int s) { return (int64_t)(2 * s + (s == s0 && s0 * line.share != u0 ? 1 : 0)) * a.rows + g % 16; };
+  float M = -INFINITY;
+  for (int s = s0 + (int)threadIdx.x; s <= s1; s += 256) M = fmaxf(M, a.stat[row_of(s) * 2]);
+  M = wave_max(M);
+  if (lane == 0) tops[threadIdx.x >> 6] = M;
+  __syncthreads();
+  M = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+  const float ms = M == -INFINITY ? 0.f : M;
+  f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+  float L = 0.f;
+#pragma unroll 4
+  for (int s = s0 + part; s <= s1; s += PARTS) {
+    const int64_t row = row_of(s);
+    const float f = __builtin_amdgcn_exp2f(a.stat[row * 2] - ms);
+    const f32x4 x = *reinterpret_cast<const f32x4*>(a.part + row * DH + 4 * d4);
+    L = fmaf(f, a.stat[row * 2 + 1], L);
 #pragma unroll
-    for (int d = 0; d < N; ++d) sum[d] = fmaf(sum[d], old, f * a.part[at * DH + N * lane + d]);
+    for (int e = 0; e < 4; ++e) sum[e] = fmaf(f, x[e], sum[e]);
+  }
+  sums[part][d4] = sum;
+  if (d4 == 0) weight[part] = L;
+  __syncthreads();
+  if (part > 0) return;
+#pragma unroll
+  for (int p = 1; p < PARTS; ++p) {
+    L += weight[p];
+    const f32x4 x = sums[p][d4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sum[e] += x[e];
   }
   const float inv = L == 0.f ? 0.f : 1.f / L;
-#pragma unroll
-  for (int d = 0; d < N; ++d) reinterpret_cast<uint16_t*>(y)[N * lane + d] = (uint16_t)pack_bf16x2(sum[d] * inv, 0.f);
+  *reinterpret_cast<uint2*>(y + d4 * 8) = make_uint2(pack_bf16x2(sum[0] * inv, sum[1] * inv), pack_bf16x2(sum[2] * inv, sum[3] * inv));
 }
 
 // ------------------------------------------------------------------------------------------
@@ -510,18 +562,25 @@ int check_rows(const spt_cache_shape_t* s, int32_t T, const void* K, const void*
   return SPT_OK;
 }
 
-// Workgroups of the decoding launch: as many as are resident at once.
-int decode_workgroups(const spt_cache_shape_t& s) {
-  const int row = s.format == SPT_CACHE_E4M3 ? s.dh : 2 * s.dh;
-  return 256 * (row == 256 ? 1 : row == 128 ? 2 : 4);
+// Calls f with the sizes of a shape's decoding kernel.
+template <class F>
+auto with_tile(const spt_cache_shape_t& s, int H, F f) {
+  const bool e4m3 = s.format == SPT_CACHE_E4M3, one = H / s.Hk <= kQueryRows[s.dh == 128];
+  if (s.dh == 128) {
+    if (e4m3) return one ? f(DecodeTile<128, true, 1>()) : f(DecodeTile<128, true, 4>());
+    return one ? f(DecodeTile<128, false, 1>()) : f(DecodeTile<128, false, 4>());
+  }
+  if (e4m3) return one ? f(DecodeTile<64, true, 1>()) : f(DecodeTile<64, true, 2>());
+  return one ? f(DecodeTile<64, false, 1>()) : f(DecodeTile<64, false, 2>());
 }
 
-struct DecodeWorkspace { int sets, rows; size_t part, bytes; };
+struct DecodeWorkspace { int sets, rows, workgroups; size_t part, bytes; };
 DecodeWorkspace plan_decode(const spt_cache_shape_t& s, int H) {
   const int G = H / s.Hk, rows = G < 16 ? G : 16;
-  const size_t slots = 2 * (size_t)decode_workgroups(s) * rows;
+  const int workgroups = 256 * with_tile(s, H, [](auto t) { return decltype(t)::PER_CU; });   // as many as are resident at once
+  const size_t slots = 2 * (size_t)workgroups * kDecodeWaves * rows;
   const size_t part = align256(slots * s.dh * sizeof(float));
-  return {(G + 15) / 16, rows, part, part + align256(slots * 2 * sizeof(float))};
+  return {(G + 15) / 16, rows, workgroups, part, part + align256(slots * 2 * sizeof(float))};
 }
 
 int check_decode(const spt_cache_shape_t* s, int32_t H) {
@@ -534,19 +593,18 @@ int check_decode(const spt_cache_shape_t* s, int32_t H) {
   return SPT_OK;
 }
 
-template <int DH, bool E4M3>
-hipError_t launch_decode(const DecodeArgs& a, hipStream_t st) {
-  typedef DecodeTile<DH, E4M3> T;
-  constexpr int join = kDecodeWaves * 16 * (2 + DH + 4) * 4, smem = kDecodeWaves * T::RING > join ? kDecodeWaves * T::RING : join;
+template <int DH, bool E4M3, int QC>
+hipError_t launch_decode(DecodeTile<DH, E4M3, QC>, const DecodeArgs& a, hipStream_t st) {
+  constexpr int smem = DecodeTile<DH, E4M3, QC>::SMEM;
   static std::atomic<uint64_t> done{0};
-  if (const hipError_t e = allow_smem(reinterpret_cast<const void*>(decode_kernel<DH, E4M3>), smem, done); e != hipSuccess) return e;
+  if (const hipError_t e = allow_smem(reinterpret_cast<const void*>(decode_kernel<DH, E4M3, QC>), smem, done); e != hipSuccess) return e;
   {
     ScopedKernelTimer timer(kSlotAttnDecode, st);
-    hipLaunchKernelGGL((decode_kernel<DH, E4M3>), dim3(a.workgroups), dim3(64 * kDecodeWaves), smem, st, a);
+    hipLaunchKernelGGL((decode_kernel<DH, E4M3, QC>), dim3(a.workgroups), dim3(64 * kDecodeWaves), smem, st, a);
   }
-  if (const hipError_t e2 = hipGetLastError(); e2 != hipSuccess) return e2;
+  if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   ScopedKernelTimer timer(kSlotAttnDecodeJoin, st);
-  hipLaunchKernelGGL(decode_join_kernel<DH>, dim3((a.c.B * a.H + 3) / 4), dim3(256), 0, st, a);
+  hipLaunchKernelGGL(decode_join_kernel<DH>, dim3(a.c.B * a.H), dim3(256), 0, st, a);
   return hipGetLastError();
 }
 
@@ -614,11 +672,9 @@ extern "C" int spt_attn_decode(const spt_cache_shape_t* shape, int32_t H, float 
   a.part = static_cast<float*>(ws);
   a.stat = reinterpret_cast<float*>(static_cast<char*>(ws) + w.part);
   a.H = H; a.G = H / s.Hk; a.sets = w.sets; a.rows = w.rows;
-  a.workgroups = decode_workgroups(s);
+  a.workgroups = w.workgroups;
   a.cs = scale * kLog2e;
   const hipStream_t st = static_cast<hipStream_t>(stream);
-  const bool e4m3 = s.format == SPT_CACHE_E4M3;
-  const hipError_t e = s.dh == 128 ? (e4m3 ? launch_decode<128, true>(a, st) : launch_decode<128, false>(a, st))
-                                   : (e4m3 ? launch_decode<64, true>(a, st) : launch_decode<64, false>(a, st));
+  const hipError_t e = with_tile(s, H, [&](auto t) { return launch_decode(t, a, st); });
   return e == hipSuccess ? SPT_OK : SPT_ERR_HIP;
 }
