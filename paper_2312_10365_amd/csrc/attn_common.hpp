@@ -270,6 +270,11 @@ __device__ __forceinline__ bf16x8 pack8(const float* x) {
   return as_bf16x8(u32x4{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7])});
 }
 
+// The two halves of a word, as bf16, and c.
+__device__ __forceinline__ float sum2(uint32_t w, float c) {
+  return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w), __builtin_bit_cast(bf16x2, 0x3F803F80u), c, false);
+}
+
 // Whether any of the bf16 looked at was infinite or NaN: the largest magnitude, two halves at a time.
 struct NotFinite {
   typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));

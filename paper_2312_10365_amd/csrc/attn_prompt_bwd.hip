@@ -133,7 +133,7 @@ __global__ __launch_bounds__(256, 2) void prompt_bwd_q_kernel(const BwdArgs a) {
   for (int d = 0; d < DT; ++d)
 #pragma unroll
     for (int r = 0; r < 16; ++r) o[d][r] = mean[d][r] = 0.f;
-  float left_over = 0.f;                                 // sum of dS: what D lacks
+  float left_over = 0.f, rounded = 0.f;                  // sum of dS: what D lacks; of dS as rounded
   NotFinite not_finite;
 
   auto first_products = [&](int t, f32x16& s, f32x16& dp) {
@@ -169,6 +169,7 @@ __global__ __launch_bounds__(256, 2) void prompt_bwd_q_kernel(const BwdArgs a) {
       left_over += d0 + d1;
       w.p[r >> 3][(r & 7) >> 1] = pack_bf16x2(p0, p1);
       w.ds[r >> 3][(r & 7) >> 1] = pack_bf16x2(d0, d1);
+      rounded = sum2(w.ds[r >> 3][(r & 7) >> 1], rounded);
     }
     return w;
   };
@@ -203,6 +204,7 @@ __global__ __launch_bounds__(256, 2) void prompt_bwd_q_kernel(const BwdArgs a) {
     second_products(t, weights(t, s, dp, masked));
   }
   left_over += other_half(left_over);
+  rounded += other_half(rounded);
   const int64_t stat = (int64_t)head * a.Tq;
   // rows that not all queries may see hold infinities or NaN: 0 times those is NaN
   if (full < ntile * kTile && __syncthreads_or(not_finite.found())) {
@@ -228,7 +230,7 @@ __global__ __launch_bounds__(256, 2) void prompt_bwd_q_kernel(const BwdArgs a) {
   for (int d = 0; d < DT; ++d) {
     float v[16];
 #pragma unroll
-    for (int r = 0; r < 16; ++r) v[r] = fmaf(-left_over, mean[d][r], o[d][r]) * a.scale;
+    for (int r = 0; r < 16; ++r) v[r] = fmaf(-rounded, mean[d][r], o[d][r]) * a.scale;
     *reinterpret_cast<bf16x8*>(dq + d * 64) = pack8(v);
     *reinterpret_cast<bf16x8*>(dq + d * 64 + 16) = pack8(v + 8);
   }
