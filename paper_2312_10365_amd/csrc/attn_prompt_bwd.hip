@@ -33,8 +33,20 @@ struct BwdArgs {
 // exp2 argument's subtrahend of a row: rows without a key have lse = -inf and p = 0
 __device__ __forceinline__ float row_offset(float lse) { return lse == -INFINITY ? INFINITY : lse * kLog2e; }
 
-// P and dS of 32 x 32 pairs as operands of the second products: a lane's results 8 half .. 8 half + 7.
+// P and dS of 32 x 32 pairs as operands of the second products: a lane's results 8 half .. 8 half + 7.  EXACT: dS is the sum of two bf16.
+template <bool EXACT>
 struct Weights { u32x4 p[2], ds[2]; };
+template <>
+struct Weights<true> { u32x4 p[2], ds[2], rest[2]; };
+
+// Where sequences are short, a rounding of one dS is in a whole row of a gradient, and memory takes as long as the products do; where there
+// are few rows in all, a gradient's error is that of a few of them, and the launch takes as long as it does.  dS is then exact.
+// Error of dK against 64 bits as a multiple of that of rounding it once, shapes drawn: 1.7 for sequences of two tokens, 1.5 for
+// up to 80, 1.45 for longer ones, 1.0 exact.  Key side, us, rounded and exact: 8192 tokens, 32 heads of 128 on 8: sequences of 32 95 and 99,
+// of 64 71 and 75, of 128 61 and 65; 32 heads of 64: 57 and 58, 44 and 47, 46 and 48, of 512 67 and 76.
+constexpr int kFewRows = 128;     // of queries of a sequence and key head, on average
+constexpr int kFewInAll = 8192;   // of queries and heads
+
 
 // p and dS of one pair, from its rows in memory.
 struct PairGrad { float p, ds; };
@@ -77,7 +89,7 @@ __device__ __forceinline__ void slow_dq_row(const BwdArgs& a, const char* q, con
   for (int d = 0; d < DH / 64; ++d) reinterpret_cast<uint16_t*>(dq)[lane + 64 * d] = (uint16_t)pack_bf16x2(acc[d] * a.scale, 0.f);
 }
 
-template <int DH>
+template <int DH, bool EXACT>
 __global__ __launch_bounds__(256, 2) void prompt_bwd_q_kernel(const BwdArgs a) {
   constexpr int KS = DH / 16, DT = DH / 32, TILE_BYTES = kTile * DH * 2;
   // 128-wide heads: dY of the wavefront's rows stays in LDS, or two wavefronts would not fit into a SIMD's registers
@@ -162,18 +174,20 @@ __global__ __launch_bounds__(256, 2) void prompt_bwd_q_kernel(const BwdArgs a) {
         dp[r] = sees ? dp[r] : 0.f;
       }
     }
-    Weights w;
+    Weights<EXACT> w;
 #pragma unroll
     for (int r = 0; r < 16; r += 2) {
       const float p0 = __builtin_amdgcn_exp2f(s[r]), p1 = __builtin_amdgcn_exp2f(s[r + 1]), d0 = p0 * dp[r], d1 = p1 * dp[r + 1];
       left_over += d0 + d1;
+      const uint32_t d = pack_bf16x2(d0, d1);
       w.p[r >> 3][(r & 7) >> 1] = pack_bf16x2(p0, p1);
-      w.ds[r >> 3][(r & 7) >> 1] = pack_bf16x2(d0, d1);
-      rounded = sum2(w.ds[r >> 3][(r & 7) >> 1], rounded);
+      w.ds[r >> 3][(r & 7) >> 1] = d;
+      if constexpr (EXACT) w.rest[r >> 3][(r & 7) >> 1] = pack_bf16x2(d0 - lo_bf16(d), d1 - hi_bf16(d));
+      else rounded = sum2(d, rounded);
     }
     return w;
   };
-  auto second_products = [&](int t, const Weights& w) {
+  auto second_products = [&](int t, const Weights<EXACT>& w) {
     const uint32_t kt = tiles + (t % kRing) * 2 * TILE_BYTES;
     lds.fresh();
 #pragma unroll
@@ -182,6 +196,7 @@ __global__ __launch_bounds__(256, 2) void prompt_bwd_q_kernel(const BwdArgs a) {
       for (int d = 0; d < DT; ++d) {
         const bf16x8 f = lds.columns(kt, half, d);
         o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, as_bf16x8(w.ds[half]), o[d], 0, 0, 0);
+        if constexpr (EXACT) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, as_bf16x8(w.rest[half]), o[d], 0, 0, 0);
         mean[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, as_bf16x8(w.p[half]), mean[d], 0, 0, 0);
       }
   };
@@ -204,7 +219,7 @@ __global__ __launch_bounds__(256, 2) void prompt_bwd_q_kernel(const BwdArgs a) {
     second_products(t, weights(t, s, dp, masked));
   }
   left_over += other_half(left_over);
-  rounded += other_half(rounded);
+  rounded = EXACT ? left_over : rounded + other_half(rounded);
   const int64_t stat = (int64_t)head * a.Tq;
   // rows that not all queries may see hold infinities or NaN: 0 times those is NaN
   if (full < ntile * kTile && __syncthreads_or(not_finite.found())) {
@@ -277,7 +292,7 @@ struct KvSizes {
   static_assert(GROUPS == 1 || GROUPS * RING >= 4 * DH * 32 * 4, "a gradient of the second group passes through LDS");
 };
 
-template <int DH, int GROUPS>
+template <int DH, int GROUPS, bool EXACT>
 __global__ __launch_bounds__(256 * GROUPS, 2) void prompt_bwd_kv_kernel(const BwdArgs a) {
   typedef KvSizes<DH, GROUPS> Sizes;
   constexpr int KS = DH / 16, DT = DH / 32, TILE_BYTES = Sizes::TILE_BYTES;
@@ -396,16 +411,18 @@ __global__ __launch_bounds__(256 * GROUPS, 2) void prompt_bwd_kv_kernel(const Bw
         dp[r] = sees ? dp[r] : 0.f;
       }
     }
-    Weights w;
+    Weights<EXACT> w;
 #pragma unroll
     for (int r = 0; r < 16; r += 2) {
-      const float p0 = __builtin_amdgcn_exp2f(s[r]), p1 = __builtin_amdgcn_exp2f(s[r + 1]);
+      const float p0 = __builtin_amdgcn_exp2f(s[r]), p1 = __builtin_amdgcn_exp2f(s[r + 1]), d0 = p0 * dp[r], d1 = p1 * dp[r + 1];
+      const uint32_t d = pack_bf16x2(d0, d1);
       w.p[r >> 3][(r & 7) >> 1] = pack_bf16x2(p0, p1);
-      w.ds[r >> 3][(r & 7) >> 1] = pack_bf16x2(p0 * dp[r], p1 * dp[r + 1]);
+      w.ds[r >> 3][(r & 7) >> 1] = d;
+      if constexpr (EXACT) w.rest[r >> 3][(r & 7) >> 1] = pack_bf16x2(d0 - lo_bf16(d), d1 - hi_bf16(d));
     }
     return w;
   };
-  auto second_products = [&](int buf, const Weights& w) {
+  auto second_products = [&](int buf, const Weights<EXACT>& w) {
     const uint32_t qt = tiles + buf * 2 * TILE_BYTES;
     lds.fresh();
 #pragma unroll
@@ -413,7 +430,9 @@ __global__ __launch_bounds__(256 * GROUPS, 2) void prompt_bwd_kv_kernel(const Bw
 #pragma unroll
       for (int d = 0; d < DT; ++d) {
         ov[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lds.columns(qt + TILE_BYTES, half, d), as_bf16x8(w.p[half]), ov[d], 0, 0, 0);
-        ok[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lds.columns(qt, half, d), as_bf16x8(w.ds[half]), ok[d], 0, 0, 0);
+        const bf16x8 q = lds.columns(qt, half, d);
+        ok[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(q, as_bf16x8(w.ds[half]), ok[d], 0, 0, 0);
+        if constexpr (EXACT) ok[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(q, as_bf16x8(w.rest[half]), ok[d], 0, 0, 0);
       }
   };
   for (int t0 = 0; t0 < steps; t0 += GROUPS) {
@@ -510,12 +529,12 @@ __global__ __launch_bounds__(256 * GROUPS, 2) void prompt_bwd_kv_kernel(const Bw
   }
 }
 
-template <int DH, int GROUPS>
+template <int DH, int GROUPS, bool EXACT>
 hipError_t launch_kv(const BwdArgs& a, int grid, hipStream_t st) {
   constexpr int smem = KvSizes<DH, GROUPS>::SMEM;
   static std::atomic<uint64_t> done{0};
-  if (const hipError_t e = allow_smem(reinterpret_cast<const void*>(prompt_bwd_kv_kernel<DH, GROUPS>), smem, done); e != hipSuccess) return e;
-  hipLaunchKernelGGL((prompt_bwd_kv_kernel<DH, GROUPS>), dim3(grid), dim3(256 * GROUPS), smem, st, a);
+  if (const hipError_t e = allow_smem(reinterpret_cast<const void*>(prompt_bwd_kv_kernel<DH, GROUPS, EXACT>), smem, done); e != hipSuccess) return e;
+  hipLaunchKernelGGL((prompt_bwd_kv_kernel<DH, GROUPS, EXACT>), dim3(grid), dim3(256 * GROUPS), smem, st, a);
   return hipGetLastError();
 }
 
@@ -550,16 +569,19 @@ extern "C" int spt_attn_prompt_bwd(const spt_attn_shape_t* shape, const void* Q,
   a.causal = s.causal;
   a.scale = s.scale;
   a.c = s.scale * kLog2e;
+  const bool few = (int64_t)s.Tq * a.G <= (int64_t)kFewRows * s.B || (int64_t)s.Tq * s.H <= kFewInAll;
   const hipStream_t st = static_cast<hipStream_t>(stream);
   {
     ScopedKernelTimer timer(kSlotAttnBwdQ, st);
     const int grid = head_item_grid(s.Hk, ((s.Tq >> (7 - a.hshift)) + s.B) * (a.G >> a.hshift));
-    if (s.dh == 128) hipLaunchKernelGGL(prompt_bwd_q_kernel<128>, dim3(grid), dim3(256), 0, st, a);
-    else hipLaunchKernelGGL(prompt_bwd_q_kernel<64>, dim3(grid), dim3(256), 0, st, a);
+    const auto kernel = s.dh == 128 ? (few ? prompt_bwd_q_kernel<128, true> : prompt_bwd_q_kernel<128, false>)
+                                    : (few ? prompt_bwd_q_kernel<64, true> : prompt_bwd_q_kernel<64, false>);
+    hipLaunchKernelGGL(kernel, dim3(grid), dim3(256), 0, st, a);
     if (hipGetLastError() != hipSuccess) return SPT_ERR_HIP;
   }
   ScopedKernelTimer timer(kSlotAttnBwdKV, st);
   const int grid = head_item_grid(s.Hk, s.Tk / kOwnKeys + s.B);
-  const hipError_t e = s.dh == 128 ? launch_kv<128, 2>(a, grid, st) : launch_kv<64, 1>(a, grid, st);
+  const hipError_t e = s.dh == 128 ? (few ? launch_kv<128, 2, true>(a, grid, st) : launch_kv<128, 2, false>(a, grid, st))
+                                   : (few ? launch_kv<64, 1, true>(a, grid, st) : launch_kv<64, 1, false>(a, grid, st));
   return e == hipSuccess ? SPT_OK : SPT_ERR_HIP;
 }
