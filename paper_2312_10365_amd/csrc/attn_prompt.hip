@@ -53,11 +53,14 @@ __device__ __forceinline__ void slow_row(const char* q, const char* k, int64_t k
   if (lse && lane == 0) *lse = (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
-template <int DH>
-__global__ __launch_bounds__(256, 2) void prompt_fwd_kernel(const FwdArgs a) {
-  constexpr int KS = DH / 16, DT = DH / 32, TILE_BYTES = kTileKeys * DH * 2;
-  __shared__ __align__(256) char smem[4 * TILE_BYTES];   // K, V, twice
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 31, h = lane >> 5;
+// GROUPS: groups of four wavefronts that go through every GROUPS-th tile of keys for the same queries.
+template <int DH, int GROUPS>
+__global__ __launch_bounds__(256 * GROUPS, 2) void prompt_fwd_kernel(const FwdArgs a) {
+  constexpr int KS = DH / 16, DT = DH / 32, TILE_BYTES = kTileKeys * DH * 2, RING = 4 * TILE_BYTES;   // K, V, twice
+  extern __shared__ __align__(256) char smem[];
+  const int lane = threadIdx.x & 63, i = lane & 31, h = lane >> 5, tid = threadIdx.x & 255;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) & 3, group = GROUPS == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 8);
+  char* ring = smem + group * RING;
 
   const int hsets = a.G >> a.hshift, pshift = 7 - a.hshift;               // 1 << pshift positions of a workgroup
   const HeadItem w = head_item(blockIdx.x, a.Hk);
@@ -80,7 +83,7 @@ __global__ __launch_bounds__(256, 2) void prompt_fwd_kernel(const FwdArgs a) {
 
   // the wavefront's queries, through the second ring buffer: whole lines
   const char* qbase = a.Q.p + (int64_t)sq.first * a.Q.row + (int64_t)head * a.Q.head;
-  const uint32_t tiles = lds_addr(smem), mine_lds = 2 * TILE_BYTES + wave * (32 * DH * 2);
+  const uint32_t tiles = lds_addr(ring), mine_lds = 2 * TILE_BYTES + wave * (32 * DH * 2);
   fetch_rows<DH>(qbase + min(i0, nq - 1) * a.Q.row, a.Q.row, max(nq - i0, 1), tiles + mine_lds, lane);
   const char* kbase = a.K.p + (int64_t)sk.first * a.K.row + (int64_t)hk * a.K.head;
   const char* vbase = a.V.p + (int64_t)sk.first * a.V.row + (int64_t)hk * a.V.head;
@@ -92,10 +95,10 @@ __global__ __launch_bounds__(256, 2) void prompt_fwd_kernel(const FwdArgs a) {
     const char* vb = vbase + (int64_t)j0 * a.V.row;
 #pragma unroll
     for (int u = 0; u < COPIES; ++u) {
-      const int slot = u * 256 + (int)threadIdx.x, row = slot / (DH / 8);
+      const int slot = u * 256 + tid, row = slot / (DH / 8);
       const uint32_t chunk = ((slot % (DH / 8)) ^ row_swizzle<DH>(row)) * 16;
       const uint32_t r = (uint32_t)min(row, nk - 1 - j0);               // (rows past the end: the last one again)
-      const uint32_t at = lds_addr(smem + buf * 2 * TILE_BYTES + u * 4096 + wave * 1024);
+      const uint32_t at = lds_addr(ring + buf * 2 * TILE_BYTES + u * 4096 + wave * 1024);
       dma16_at(kb, r * (uint32_t)a.K.row + chunk, at);
       dma16_at(vb, r * (uint32_t)a.V.row + chunk, at + TILE_BYTES);
     }
@@ -109,21 +112,22 @@ __global__ __launch_bounds__(256, 2) void prompt_fwd_kernel(const FwdArgs a) {
   float m = -INFINITY, neg_m = 0.f, l = 0.f;
   NotFinite not_finite;
 
-  if (ntile > 0) fetch(0, 0);
+  if (group < ntile) fetch(group, 0);
   bf16x8 qf[KS];
-  if (ntile > 0) wait_vmcnt<2 * COPIES>();
+  if (group < ntile) wait_vmcnt<2 * COPIES>();
   else wait_vmcnt<0>();
 #pragma unroll
   for (int s = 0; s < KS; ++s) qf[s] = lds.rows(tiles + mine_lds, 0, s);
-  for (int t = 0; t < ntile; ++t) {
+  for (int t0 = 0; t0 < ntile; t0 += GROUPS) {
     wait_vmcnt<0>();
     __syncthreads();
-    if (t + 1 < ntile) fetch(t + 1, (t + 1) & 1);
-    const int j0 = t * kTileKeys;
-    const uint32_t kt_ = tiles + (t & 1) * 2 * TILE_BYTES, vt_ = kt_ + TILE_BYTES;
+    const int t = t0 + group, buf = t0 / GROUPS & 1, j0 = t * kTileKeys;
+    if (t + GROUPS < ntile) fetch(t + GROUPS, buf ^ 1);
+    if (t >= ntile) continue;
+    const uint32_t kt_ = tiles + buf * 2 * TILE_BYTES, vt_ = kt_ + TILE_BYTES;
     if (j0 + kTileKeys > full) {
 #pragma unroll
-      for (int u = 0; u < TILE_BYTES / 4096; ++u) not_finite.look(lds_read<u32x4>(vt_ + u * 4096 + threadIdx.x * 16));
+      for (int u = 0; u < TILE_BYTES / 4096; ++u) not_finite.look(lds_read<u32x4>(vt_ + u * 4096 + tid * 16));
     }
     if (j0 >= wave_kend) continue;
     lds.fresh();
@@ -183,7 +187,7 @@ __global__ __launch_bounds__(256, 2) void prompt_fwd_kernel(const FwdArgs a) {
   float* lse = a.lse ? a.lse + (int64_t)head * a.Tq + sq.first : nullptr;
   // rows of V that not all queries may see hold infinities or NaN: 0 times those is NaN
   if (full < ntile * kTileKeys && __syncthreads_or(not_finite.found())) {
-    for (int r = 0; r < min(32, nq - i0); ++r) {
+    for (int r = group; r < min(32, nq - i0); r += GROUPS) {
       const int row = i0 + r;
       slow_row<DH>(a.Q.p + (int64_t)(sq.first + row) * a.Q.row + (int64_t)head * a.Q.head, kbase, a.K.row, vbase, a.V.row,
                    a.causal ? min(nk, row + ahead + 1) : nk, a.c, a.Y.p + (int64_t)(sq.first + row) * a.Y.row + (int64_t)head * a.Y.head,
@@ -191,12 +195,40 @@ __global__ __launch_bounds__(256, 2) void prompt_fwd_kernel(const FwdArgs a) {
     }
     return;
   }
-  if (i0 >= nq) return;
   l += other_half(l);
+  if (GROUPS == 2) {                                     // the second group's part, scaled to the larger maximum of the two
+    float* part = reinterpret_cast<float*>(smem) + wave * (DT * 1024 + 128) + lane * 4;
+    float* ml = reinterpret_cast<float*>(smem) + wave * (DT * 1024 + 128) + DT * 1024;
+    __syncthreads();
+    if (group == 1) {
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) *reinterpret_cast<f32x4*>(part + (d * 4 + q) * 256) = f32x4{o[d][4 * q], o[d][4 * q + 1], o[d][4 * q + 2], o[d][4 * q + 3]};
+      ml[lane] = m;
+      ml[64 + lane] = l;
+    }
+    __syncthreads();
+    if (group == 1) return;
+    const float m1 = ml[lane], mn = fmaxf(m, m1), ms = mn == -INFINITY ? 0.f : mn;
+    const float f0 = __builtin_amdgcn_exp2f(m - ms), f1 = __builtin_amdgcn_exp2f(m1 - ms);
+    l = fmaf(l, f0, ml[64 + lane] * f1);
+    m = mn;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const f32x4 x = *reinterpret_cast<const f32x4*>(part + (d * 4 + q) * 256);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[d][4 * q + e] = fmaf(o[d][4 * q + e], f0, x[e] * f1);
+      }
+    wave_lds_fence();
+  }
+  if (i0 >= nq) return;
   const float inv = l == 0.f ? 0.f : 1.f / l;
   if (lse && h == 0 && i0 + i < nq) lse[mine] = (m + __builtin_amdgcn_logf(l)) * kLn2;
-  // rows out as whole lines, through the ring buffer that the last tile is not in
-  const uint32_t out = (ntile & 1) * 2 * TILE_BYTES + wave * (32 * DH * 2);
+  // rows out as whole lines, through the ring buffer that the last tile is not in (two groups: where the wavefront's sums were)
+  const uint32_t out = GROUPS == 2 ? wave * (DT * 4096 + 512) : (ntile & 1) * 2 * TILE_BYTES + wave * (32 * DH * 2);
 #pragma unroll
   for (int d = 0; d < DT; ++d) {
     float v[16];
@@ -206,6 +238,25 @@ __global__ __launch_bounds__(256, 2) void prompt_fwd_kernel(const FwdArgs a) {
   }
   wave_lds_fence();
   store_rows<DH>(smem + out, a.Y.p + (int64_t)(sq.first + i0) * a.Y.row + (int64_t)head * a.Y.head, a.Y.row, nq - i0, lane);
+}
+
+// Two groups of wavefronts a workgroup where the chip would not be full: with no more workgroups than are resident at once (two on a CU at
+// dh 128; at dh 64 four, of which three count) the one with the most keys is what the launch waits for.  us, one group and two, 32 heads on 8 of
+// 128: one sequence of 2048 56.6 and 49.2, 512 queries behind 4000 keys 98.7 and 75.7, four parts of 512 behind 700 to 5000 146 and 129;
+// of 4096 (twice as many as are resident) 154 and 158; four of 512, which have few tiles to share, 23.0 and 26.2, one of them 17.5 and 16.4; 12
+// heads of 64, one of 1000 21.2 and 17.1, of 8000 146 and 133; 32 heads of 64, four of 1024 (four workgroups on a CU) 33 and 37.
+bool two_groups(const spt_attn_shape_t& s, int hshift) {
+  const int64_t workgroups = (int64_t)(s.Tq >> (7 - hshift)) * (s.H >> hshift), resident = 256 * (s.dh == 128 ? 2 : 3);
+  return workgroups <= resident / 2 || (workgroups <= resident && s.Tk >= 1024 * (int64_t)s.B);
+}
+
+template <int DH, int GROUPS>
+hipError_t launch_fwd(const FwdArgs& a, int grid, hipStream_t st) {
+  constexpr int smem = GROUPS * 4 * kTileKeys * DH * 2;
+  static std::atomic<uint64_t> done{0};
+  if (const hipError_t e = allow_smem(reinterpret_cast<const void*>(prompt_fwd_kernel<DH, GROUPS>), smem, done); e != hipSuccess) return e;
+  hipLaunchKernelGGL((prompt_fwd_kernel<DH, GROUPS>), dim3(grid), dim3(256 * GROUPS), smem, st, a);
+  return hipGetLastError();
 }
 
 }  // namespace
@@ -248,7 +299,8 @@ extern "C" int spt_attn_prompt_fwd(const spt_attn_shape_t* shape, const void* Q,
   a.c = s.scale * kLog2e;
   const hipStream_t st = static_cast<hipStream_t>(stream);
   ScopedKernelTimer timer(kSlotAttnFwd, st);
-  if (s.dh == 128) hipLaunchKernelGGL(prompt_fwd_kernel<128>, dim3(grid), dim3(256), 0, st, a);
-  else hipLaunchKernelGGL(prompt_fwd_kernel<64>, dim3(grid), dim3(256), 0, st, a);
-  return hipGetLastError() == hipSuccess ? SPT_OK : SPT_ERR_HIP;
+  const bool two = two_groups(s, a.hshift);
+  const hipError_t e = s.dh == 128 ? (two ? launch_fwd<128, 2>(a, grid, st) : launch_fwd<128, 1>(a, grid, st))
+                                   : (two ? launch_fwd<64, 2>(a, grid, st) : launch_fwd<64, 1>(a, grid, st));
+  return e == hipSuccess ? SPT_OK : SPT_ERR_HIP;
 }
