@@ -98,7 +98,6 @@ def alloc_decode_workspace(shape: CacheShape, H: int, device="cuda") -> torch.Te
 
 _BF16, _F32, _I32, _U8 = torch.bfloat16, torch.float32, torch.int32, torch.uint8
 _byref = ctypes.byref
-_strides2, _strides4, _strides8 = (ctypes.c_int64 * 4), (ctypes.c_int64 * 8), (ctypes.c_int64 * 16)
 
 
 def _gpu(t, name: str) -> int:
@@ -118,21 +117,24 @@ def _dense(t, dtype, numel: int, dev: int, name: str):
     return t.data_ptr()
 
 
-def _rows(t, shape, dev: int, name: str):
-    """Pointer of rows [T, heads, dh], which may lie apart."""
-    if t.dtype is not _BF16 or t.shape != shape or t.get_device() != dev or t.stride(2) != 1:
-        raise ValueError(f"{name}: need a tensor of {_BF16} {shape} on cuda:{dev} with a dense last axis, "
-                         f"got {t.dtype} {tuple(t.shape)} on {t.device}, strides {tuple(t.stride())}")
-    return t.data_ptr()
+def _rows(t, shape, dev: int, name: str, apart: list):
+    """Pointer of rows [T, heads, dh], which may lie apart: then their name goes into `apart`."""
+    if t.dtype is _BF16 and t.shape == shape and t.get_device() == dev:
+        if t.is_contiguous():
+            return t.data_ptr()
+        if t.stride(2) == 1:
+            apart.append(name)
+            return t.data_ptr()
+    raise ValueError(f"{name}: need a tensor of {_BF16} {shape} on cuda:{dev} with a dense last axis, "
+                     f"got {t.dtype} {tuple(t.shape)} on {t.device}, strides {tuple(t.stride())}")
 
 
-def _strides(kind, *tensors):
-    """Row and head strides of tensors, or None where all are dense."""
-    for t in tensors:
-        if not t.is_contiguous():
-            return kind(*(n for t in tensors for n in ((t.stride(0), t.stride(1)) if not t.is_contiguous() else
-                                                       (t.shape[1] * t.shape[2], t.shape[2]))))
-    return None
+def _strides(apart: list, *tensors):
+    """Row and head strides of all row tensors of a call, or None where all are dense."""
+    if not apart:
+        return None
+    at = [n for t in tensors for n in ((t.shape[1] * t.shape[2], t.shape[2]) if t.is_contiguous() else (t.stride(0), t.stride(1)))]
+    return (ctypes.c_int64 * len(at))(*at)
 
 
 def _call(dev: int, name: str, *args):
@@ -160,9 +162,11 @@ def prompt_fwd(shape: AttnShape, Q, K, V, cu_q, cu_k, Y=None, lse=None, save_for
         Y = torch.empty(q, dtype=_BF16, device=Q.device)
     if lse is None and save_for_backward:
         lse = torch.empty((H, Tq), dtype=_F32, device=Q.device)
-    _call(dev, "spt_attn_prompt_fwd", _byref(s), _rows(Q, q, dev, "Q"), _rows(K, k, dev, "K"), _rows(V, k, dev, "V"),
-          _strides(_strides4, Q, K, V, Y), _dense(cu_q, _I32, B + 1, dev, "cu_q"), _dense(cu_k, _I32, B + 1, dev, "cu_k"),
-          _rows(Y, q, dev, "Y"), _dense(lse, _F32, H * Tq, dev, "lse"))
+    apart = []
+    y = _rows(Y, q, dev, "Y", apart)
+    _call(dev, "spt_attn_prompt_fwd", _byref(s), _rows(Q, q, dev, "Q", apart), _rows(K, k, dev, "K", apart), _rows(V, k, dev, "V", apart),
+          _strides(apart, Q, K, V, Y), _dense(cu_q, _I32, B + 1, dev, "cu_q"), _dense(cu_k, _I32, B + 1, dev, "cu_k"), y,
+          _dense(lse, _F32, H * Tq, dev, "lse"))
     return Y, lse
 
 
@@ -174,10 +178,12 @@ def prompt_bwd(shape: AttnShape, Q, K, V, Y, dY, lse, cu_q, cu_k, ws=None, dQ=No
     dQ, dK, dV = (torch.empty(n, dtype=_BF16, device=Q.device) if t is None else t for t, n in ((dQ, q), (dK, k), (dV, k)))
     if ws is None:
         ws = alloc_prompt_workspace(s, Q.device)
-    _call(dev, "spt_attn_prompt_bwd", _byref(s), _rows(Q, q, dev, "Q"), _rows(K, k, dev, "K"), _rows(V, k, dev, "V"), _rows(Y, q, dev, "Y"),
-          _rows(dY, q, dev, "dY"), _dense(lse, _F32, H * Tq, dev, "lse"), _strides(_strides8, Q, K, V, Y, dY, dQ, dK, dV),
-          _dense(cu_q, _I32, B + 1, dev, "cu_q"), _dense(cu_k, _I32, B + 1, dev, "cu_k"), _rows(dQ, q, dev, "dQ"), _rows(dK, k, dev, "dK"),
-          _rows(dV, k, dev, "dV"), _dense(ws, _U8, ws.numel(), dev, "ws"), ws.numel())
+    apart = []
+    dq, dk, dv = _rows(dQ, q, dev, "dQ", apart), _rows(dK, k, dev, "dK", apart), _rows(dV, k, dev, "dV", apart)
+    _call(dev, "spt_attn_prompt_bwd", _byref(s), _rows(Q, q, dev, "Q", apart), _rows(K, k, dev, "K", apart), _rows(V, k, dev, "V", apart),
+          _rows(Y, q, dev, "Y", apart), _rows(dY, q, dev, "dY", apart), _dense(lse, _F32, H * Tq, dev, "lse"),
+          _strides(apart, Q, K, V, Y, dY, dQ, dK, dV), _dense(cu_q, _I32, B + 1, dev, "cu_q"), _dense(cu_k, _I32, B + 1, dev, "cu_k"),
+          dq, dk, dv, _dense(ws, _U8, ws.numel(), dev, "ws"), ws.numel())
     return dQ, dK, dV
 
 
@@ -192,8 +198,8 @@ def _pool(s: CacheShape, cache, dev: int):
 
 
 def _move_rows(name: str, s: CacheShape, K, V, cache, table, start, cu, dev: int):
-    n, B = (K.shape[0], s.Hk, s.dh), s.B
-    _call(dev, name, _byref(s), n[0], _rows(K, n, dev, "K"), _rows(V, n, dev, "V"), _strides(_strides2, K, V),
+    n, B, apart = (K.shape[0], s.Hk, s.dh), s.B, []
+    _call(dev, name, _byref(s), n[0], _rows(K, n, dev, "K", apart), _rows(V, n, dev, "V", apart), _strides(apart, K, V),
           _dense(table, _I32, B * s.max_pages, dev, "table"), _dense(start, _I32, B, dev, "start"), _dense(cu, _I32, B + 1, dev, "cu"),
           *_pool(s, cache, dev))
 
@@ -227,7 +233,9 @@ def decode(shape: CacheShape, Q, cache, table, lens, scale=None, ws=None, Y=None
         Y = torch.empty(n, dtype=_BF16, device=Q.device)
     if ws is None:
         ws = alloc_decode_workspace(s, H, Q.device)
-    _call(dev, "spt_attn_decode", _byref(s), H, dh ** -0.5 if scale is None else scale, _rows(Q, n, dev, "Q"), _strides(_strides2, Q, Y),
-          *_pool(s, cache, dev), _dense(table, _I32, B * s.max_pages, dev, "table"), _dense(lens, _I32, B, dev, "lens"),
-          _rows(Y, n, dev, "Y"), _dense(ws, _U8, ws.numel(), dev, "ws"), ws.numel())
+    apart = []
+    y = _rows(Y, n, dev, "Y", apart)
+    _call(dev, "spt_attn_decode", _byref(s), H, dh ** -0.5 if scale is None else scale, _rows(Q, n, dev, "Q", apart), _strides(apart, Q, Y),
+          *_pool(s, cache, dev), _dense(table, _I32, B * s.max_pages, dev, "table"), _dense(lens, _I32, B, dev, "lens"), y,
+          _dense(ws, _U8, ws.numel(), dev, "ws"), ws.numel())
     return Y
