@@ -216,138 +216,24 @@ struct Unit {
   int page[2];                    // of its two halves
 };
 
-template <int DH, bool E4M3, int QC>
-__global__ __launch_bounds__(64 * kDecodeWaves, 2) void decode_kernel(const DecodeArgs a) {
-  typedef DecodeTile<DH, E4M3, QC> T;
-  constexpr int RB = T::RB, KS = DH / 32, DT = DH / 16;
-  extern __shared__ __align__(256) char smem[];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int q = lane & 15, c = lane >> 4, items = a.c.Hk * a.sets, qrow = min(q, QC * (512 / DH) - 1);
-  char* ring = smem + wave * T::RING;
-
-  const Line line = unit_line(a);
-  const int stretch = wave * a.workgroups + blockIdx.x;    // (few stretches: one on a CU)
-  if (stretch > line.total / line.share) return;
-  int left = min(line.total - stretch * line.share, line.share);
-  if (left <= 0) return;
-
-  auto pages_of = [&](Unit& x) {
-#pragma unroll
-    for (int half = 0; half < 2; ++half)
-      x.page[half] = uniform_load(a.c.table + (int64_t)x.b * a.c.max_pages + (min(x.t * kUnit + 16 * half, x.len - 1) >> a.c.page_shift));
-  };
-  auto sequence = [&](Unit& x) {
-    x.len = seq_len(a, uniform_load(a.lens + x.b));
-    x.units = units_of(x.len);
-  };
-  Unit ahead;                                              // the next unit to be asked for
-  {
-    const int u = stretch * line.share;
-    int before = 0, rem = 0;
-    ahead.b = 0;
-    for (int b0 = 0; b0 < a.c.B; b0 += 64) {
-      const int incl = wave_prefix(b0 + lane < a.c.B ? seq_units(a, b0 + lane) : 0) * items, total = __builtin_amdgcn_readlane(incl, 63);
-      if (u - before < total) {
-        const int src = __builtin_ctzll(__ballot(incl > u - before));
-        ahead.b = b0 + src;
-        rem = u - before - (src > 0 ? __builtin_amdgcn_readlane(incl, src - 1) : 0);
-        break;
-      }
-      before += total;
-    }
-    sequence(ahead);
-    ahead.item = rem / ahead.units;
-    ahead.t = rem - ahead.item * ahead.units;
-    pages_of(ahead);
-  }
-  auto advance = [&](Unit& x) {                            // (there is one more unit)
-    if (++x.t == x.units) {
-      x.t = 0;
-      if (++x.item == items) {
-        x.item = 0;
-        do {
-          ++x.b;
-          sequence(x);
-        } while (x.units == 0);
-      }
-    }
-    pages_of(x);
-  };
-  auto head0_of = [&](const Unit& x) { return x.item / a.sets * a.G + x.item % a.sets * 16; };
-  auto heads_of = [&](const Unit& x) { return min(16, a.G - x.item % a.sets * 16); };
-
-  // copies of a unit into a stage (with its item's queries where these are new); returns which of its 32 tokens are there
-  auto fetch = [&](const Unit& x, bool queries, int stage) -> uint32_t {
-    const uint32_t at = lds_addr(ring + stage * T::STAGE);
-    const int hk = x.item / a.sets;
-    uint32_t there = 0;
-    int64_t row[2];
-#pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      const int pos = x.t * kUnit + 16 * half;
-      const bool ok = pos < x.len && x.page[half] >= 0 && x.page[half] < a.c.pages;
-      if (ok) there |= (x.len - pos >= 16 ? 0xFFFFu : (1u << (x.len - pos)) - 1u) << (16 * half);
-      row[half] = ((((int64_t)(ok ? x.page[half] : 0) * a.c.Hk) + hk) << a.c.page_shift) + (pos & ((1 << a.c.page_shift) - 1));
-    }
-#pragma unroll
-    for (int n = 0; n < T::COPIES; ++n) {
-      const int r = n * (1024 / RB) + lane / (RB / 16);    // row of the unit; those of a copy lie in one half
-      const int half = n * (1024 / RB) / 16;
-      const uint32_t off = (uint32_t)(r - 16 * half) * RB + (((uint32_t)lane % (RB / 16)) ^ chunk_swizzle<RB>(r)) * 16;
-      dma16_at(a.c.Kc + row[half] * RB, off, at + n * 1024);
-      dma16_at(a.c.Vc + row[half] * RB, off, at + T::BYTES + n * 1024);
-    }
-    if (E4M3) {                                            // lanes 0-7: exponents of the keys, 8-15: of the values
-      const int half = (lane >> 2) & 1;
-      dma4(((lane & 8) ? a.c.vs : a.c.ks) + row[half] + 4 * (lane & 3), at + 2 * T::BYTES + T::QUERIES);
-    }
-    if (queries) {
-      const char* base = a.Q.p + x.b * a.Q.row + (int64_t)head0_of(x) * a.Q.head;
-      const int heads = heads_of(x);
-#pragma unroll
-      for (int n = 0; n < T::QCOPIES; ++n) {
-        const int r = n * (512 / DH) + lane / (DH / 8);    // (rows past the heads: the last one again)
-        dma16_at(base, (uint32_t)min(r, heads - 1) * (uint32_t)a.Q.head + (((uint32_t)lane % (DH / 8)) ^ row_swizzle<DH>(r)) * 16,
-                 at + 2 * T::BYTES + n * 1024);
-      }
-    }
-    return there;
-  };
-
+// Up to sixteen query heads of an item (the lane's: lane % 16) over the units so far: maximum, sum (of the lane's tokens), output.
+template <int DH, bool E4M3>
+struct DecodeState {
+  static constexpr int RB = E4M3 ? DH : DH * 2, COPIES = kUnit * RB / 1024, KS = DH / 32, DT = DH / 16;
   bf16x8 qf[KS];
   f32x4 o[DT];
   float m, neg_m, l;
-  Unit now = ahead, next = ahead;
-  bool fresh = true, next_fresh = false, first_item = true;   // whether a unit's queries are new
-  int item_units = 0;                                      // units of the present item so far
-  uint32_t there = fetch(now, true, 0), next_there = 0;
-  --left;
-  if (left > 0) {
-    advance(ahead);
-    next = ahead;
-    next_fresh = next.t == 0;
-    next_there = fetch(next, next_fresh, 1);
-    if (left > 1) advance(ahead);
+
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int d = 0; d < DT; ++d) o[d] = f32x4{0.f, 0.f, 0.f, 0.f};
+    m = -INFINITY; neg_m = 0.f; l = 0.f;
   }
-  for (int stage = 0;; stage ^= 1) {
-    if (left <= 0) wait_vmcnt<0>();
-    else if (next_fresh) wait_vmcnt<T::LOADS + T::QCOPIES>();
-    else wait_vmcnt<T::LOADS>();
-    wave_lds_fence();
-    char* kt = ring + stage * T::STAGE;
-    char* vt = kt + T::BYTES;
-    if (fresh) {
-#pragma unroll
-      for (int s = 0; s < KS; ++s)
-        qf[s] = *reinterpret_cast<const bf16x8*>(kt + 2 * T::BYTES + qrow * (DH * 2) + ((uint32_t)(4 * s + c) ^ row_swizzle<DH>(qrow)) * 16);
-#pragma unroll
-      for (int d = 0; d < DT; ++d) o[d] = f32x4{0.f, 0.f, 0.f, 0.f};
-      m = -INFINITY; neg_m = 0.f; l = 0.f;
-      item_units = 0;
-    }
-    ++item_units;
+  // A unit that lies in LDS: rows kt, vt, the rows' exponents, which of its tokens are there.
+  __device__ __forceinline__ void unit(char* kt, char* vt, const char* exponents, uint32_t there, float cs, int lane) {
+    const int q = lane & 15, c = lane >> 4;
     if (there != 0xFFFFFFFFu) {                            // 0 times what lies behind the last token may be NaN
-      for (int n = 0; n < T::COPIES; ++n) {
+      for (int n = 0; n < COPIES; ++n) {
         const int r = n * (1024 / RB) + lane / (RB / 16);
         if (!((there >> r) & 1)) *reinterpret_cast<u32x4*>(vt + n * 1024 + lane * 16) = u32x4{0, 0, 0, 0};
       }
@@ -374,14 +260,14 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void decode_kernel(const Deco
     }
     uint32_t kb[2] = {0, 0}, vb[2] = {0, 0};               // exponents of the lane's tokens 16 kt2 + 4 c + e
     if (E4M3) {
-      const uint32_t* ex = reinterpret_cast<const uint32_t*>(kt + 2 * T::BYTES + T::QUERIES);
+      const uint32_t* ex = reinterpret_cast<const uint32_t*>(exponents);
       kb[0] = ex[c]; kb[1] = ex[4 + c];
       vb[0] = ex[8 + c]; vb[1] = ex[12 + c];
     }
     float x[8], top = -INFINITY;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      float v = s[e >> 2][e & 3] * a.cs;
+      float v = s[e >> 2][e & 3] * cs;
       if (E4M3) v = __builtin_ldexpf(v, (int)((kb[e >> 2] >> (8 * (e & 3))) & 255u) - 127);
       x[e] = (there >> (16 * (e >> 2) + 4 * c + (e & 3))) & 1 ? v : -INFINITY;
       top = fmaxf(top, x[e]);
@@ -434,6 +320,149 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void decode_kernel(const Deco
       o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, hi, o[d], 0, 0, 0);
       o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, lo, o[d], 0, 0, 0);
     }
+  }
+  __device__ __forceinline__ float sum() const {             // of all tokens
+    const float s = l + __shfl_xor(l, 16);
+    return s + __shfl_xor(s, 32);
+  }
+};
+
+// Asynchronous copies of unit t of a sequence into a stage; returns which of its 32 tokens are there.
+template <int DH, bool E4M3>
+__device__ __forceinline__ uint32_t fetch_unit(const DecodeArgs& a, int hk, int t, int len, const int* page, uint32_t at, uint32_t exponents, int lane) {
+  constexpr int RB = E4M3 ? DH : DH * 2, BYTES = kUnit * RB;
+  uint32_t there = 0;
+  int64_t row[2];
+#pragma unroll
+  for (int half = 0; half < 2; ++half) {
+    const int pos = t * kUnit + 16 * half;
+    const bool ok = pos < len && page[half] >= 0 && page[half] < a.c.pages;
+    if (ok) there |= (len - pos >= 16 ? 0xFFFFu : (1u << (len - pos)) - 1u) << (16 * half);
+    row[half] = ((((int64_t)(ok ? page[half] : 0) * a.c.Hk) + hk) << a.c.page_shift) + (pos & ((1 << a.c.page_shift) - 1));
+  }
+#pragma unroll
+  for (int n = 0; n < BYTES / 1024; ++n) {
+    const int r = n * (1024 / RB) + lane / (RB / 16);        // row of the unit; those of a copy lie in one half
+    const int half = n * (1024 / RB) / 16;
+    const uint32_t off = (uint32_t)(r - 16 * half) * RB + (((uint32_t)lane % (RB / 16)) ^ chunk_swizzle<RB>(r)) * 16;
+    dma16_at(a.c.Kc + row[half] * RB, off, at + n * 1024);
+    dma16_at(a.c.Vc + row[half] * RB, off, at + BYTES + n * 1024);
+  }
+  if (E4M3) {                                                // lanes 0-7: exponents of the keys, 8-15: of the values
+    const int half = (lane >> 2) & 1;
+    dma4(((lane & 8) ? a.c.vs : a.c.ks) + row[half] + 4 * (lane & 3), exponents);
+  }
+  return there;
+}
+__device__ __forceinline__ int unit_page(const DecodeArgs& a, int b, int t, int half, int len) {
+  return uniform_load(a.c.table + (int64_t)b * a.c.max_pages + (min(t * kUnit + 16 * half, len - 1) >> a.c.page_shift));
+}
+
+template <int DH, bool E4M3, int QC>
+__global__ __launch_bounds__(64 * kDecodeWaves, 2) void decode_kernel(const DecodeArgs a) {
+  typedef DecodeTile<DH, E4M3, QC> T;
+  constexpr int KS = DH / 32, DT = DH / 16;
+  extern __shared__ __align__(256) char smem[];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int q = lane & 15, c = lane >> 4, items = a.c.Hk * a.sets, qrow = min(q, QC * (512 / DH) - 1);
+  char* ring = smem + wave * T::RING;
+
+  const Line line = unit_line(a);
+  const int stretch = wave * a.workgroups + blockIdx.x;    // (few stretches: one on a CU)
+  if (stretch > line.total / line.share) return;
+  int left = min(line.total - stretch * line.share, line.share);
+  if (left <= 0) return;
+
+  auto pages_of = [&](Unit& x) {
+#pragma unroll
+    for (int half = 0; half < 2; ++half) x.page[half] = unit_page(a, x.b, x.t, half, x.len);
+  };
+  auto sequence = [&](Unit& x) {
+    x.len = seq_len(a, uniform_load(a.lens + x.b));
+    x.units = units_of(x.len);
+  };
+  Unit ahead;                                              // the next unit to be asked for
+  {
+    const int u = stretch * line.share;
+    int before = 0, rem = 0;
+    ahead.b = 0;
+    for (int b0 = 0; b0 < a.c.B; b0 += 64) {
+      const int incl = wave_prefix(b0 + lane < a.c.B ? seq_units(a, b0 + lane) : 0) * items, total = __builtin_amdgcn_readlane(incl, 63);
+      if (u - before < total) {
+        const int src = __builtin_ctzll(__ballot(incl > u - before));
+        ahead.b = b0 + src;
+        rem = u - before - (src > 0 ? __builtin_amdgcn_readlane(incl, src - 1) : 0);
+        break;
+      }
+      before += total;
+    }
+    sequence(ahead);
+    ahead.item = rem / ahead.units;
+    ahead.t = rem - ahead.item * ahead.units;
+    pages_of(ahead);
+  }
+  auto advance = [&](Unit& x) {                            // (there is one more unit)
+    if (++x.t == x.units) {
+      x.t = 0;
+      if (++x.item == items) {
+        x.item = 0;
+        do {
+          ++x.b;
+          sequence(x);
+        } while (x.units == 0);
+      }
+    }
+    pages_of(x);
+  };
+  auto head0_of = [&](const Unit& x) { return x.item / a.sets * a.G + x.item % a.sets * 16; };
+  auto heads_of = [&](const Unit& x) { return min(16, a.G - x.item % a.sets * 16); };
+
+  // copies of a unit into a stage (with its item's queries where these are new); returns which of its 32 tokens are there
+  auto fetch = [&](const Unit& x, bool queries, int stage) -> uint32_t {
+    const uint32_t at = lds_addr(ring + stage * T::STAGE);
+    const uint32_t there = fetch_unit<DH, E4M3>(a, x.item / a.sets, x.t, x.len, x.page, at, at + 2 * T::BYTES + T::QUERIES, lane);
+    if (queries) {
+      const char* base = a.Q.p + x.b * a.Q.row + (int64_t)head0_of(x) * a.Q.head;
+      const int heads = heads_of(x);
+#pragma unroll
+      for (int n = 0; n < T::QCOPIES; ++n) {
+        const int r = n * (512 / DH) + lane / (DH / 8);    // (rows past the heads: the last one again)
+        dma16_at(base, (uint32_t)min(r, heads - 1) * (uint32_t)a.Q.head + (((uint32_t)lane % (DH / 8)) ^ row_swizzle<DH>(r)) * 16,
+                 at + 2 * T::BYTES + n * 1024);
+      }
+    }
+    return there;
+  };
+
+  DecodeState<DH, E4M3> state;
+  Unit now = ahead, next = ahead;
+  bool fresh = true, next_fresh = false, first_item = true;   // whether a unit's queries are new
+  int item_units = 0;                                      // units of the present item so far
+  uint32_t there = fetch(now, true, 0), next_there = 0;
+  --left;
+  if (left > 0) {
+    advance(ahead);
+    next = ahead;
+    next_fresh = next.t == 0;
+    next_there = fetch(next, next_fresh, 1);
+    if (left > 1) advance(ahead);
+  }
+  for (int stage = 0;; stage ^= 1) {
+    if (left <= 0) wait_vmcnt<0>();
+    else if (next_fresh) wait_vmcnt<T::LOADS + T::QCOPIES>();
+    else wait_vmcnt<T::LOADS>();
+    wave_lds_fence();
+    char* kt = ring + stage * T::STAGE;
+    char* vt = kt + T::BYTES;
+    if (fresh) {
+#pragma unroll
+      for (int s = 0; s < KS; ++s)
+        state.qf[s] = *reinterpret_cast<const bf16x8*>(kt + 2 * T::BYTES + qrow * (DH * 2) + ((uint32_t)(4 * s + c) ^ row_swizzle<DH>(qrow)) * 16);
+      state.clear();
+      item_units = 0;
+    }
+    ++item_units;
+    state.unit(kt, vt, kt + 2 * T::BYTES + T::QUERIES, there, a.cs, lane);
     // the stage has been read (lgkmcnt 0: no read of it is on its way): the unit after the next one's
     wave_lds_fence();
     __builtin_amdgcn_s_waitcnt(0xC07F);
@@ -450,8 +479,8 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void decode_kernel(const Deco
       if (left > 1) advance(ahead);
     }
     if (ends) {                                            // the item's result, or the stretch's part of it
-      float sum = l + __shfl_xor(l, 16);
-      sum += __shfl_xor(sum, 32);
+      const float sum = state.sum();
+      const f32x4* o = state.o;
       const int head0 = head0_of(done);
       if (q < heads_of(done)) {
         if (item_units == done.units) {
@@ -465,7 +494,7 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void decode_kernel(const Deco
 #pragma unroll
           for (int d = 0; d < DT; ++d) *reinterpret_cast<f32x4*>(a.part + row * DH + 16 * d + 4 * c) = o[d];
           if (c == 0) {
-            a.stat[row * 2] = m;
+            a.stat[row * 2] = state.m;
             a.stat[row * 2 + 1] = sum;
           }
         }
@@ -473,6 +502,84 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void decode_kernel(const Deco
       first_item = false;
     }
     if (!more) break;
+  }
+}
+
+// Short tables: a workgroup per item, its wavefronts take turns at the units and are joined in LDS, in order: one launch.
+template <int DH, bool E4M3>
+struct ItemTile {
+  static constexpr int BYTES = kUnit * (E4M3 ? DH : DH * 2), STAGE = 2 * BYTES + (E4M3 ? 256 : 0), LOADS = 2 * (BYTES / 1024) + (E4M3 ? 1 : 0);
+  static constexpr int WAVES = STAGE >= 16384 ? 4 : 8, LD = DH + 4;
+  static constexpr int JOIN = WAVES * 16 * (LD + 2) * 4, RINGS = WAVES * 2 * STAGE, SMEM = RINGS > JOIN ? RINGS : JOIN;
+  static_assert(SMEM <= 160 * 1024, "a CU's LDS");
+};
+
+template <int DH, bool E4M3>
+__global__ __launch_bounds__((64 * ItemTile<DH, E4M3>::WAVES), 2) void decode_item_kernel(const DecodeArgs a) {
+  typedef ItemTile<DH, E4M3> T;
+  constexpr int KS = DH / 32, DT = DH / 16, WAVES = T::WAVES;
+  extern __shared__ __align__(256) char smem[];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane & 15, c = lane >> 4;
+  const int items = a.c.Hk * a.sets, b = blockIdx.x / items, item = blockIdx.x - b * items, hk = item / a.sets;
+  const int head0 = hk * a.G + item % a.sets * 16, heads = min(16, a.G - item % a.sets * 16);
+  const int len = seq_len(a, uniform_load(a.lens + b)), units = units_of(len);
+  char* ring = smem + wave * 2 * T::STAGE;
+  auto fetch = [&](int t, int stage) {
+    const int page[2] = {unit_page(a, b, t, 0, len), unit_page(a, b, t, 1, len)};
+    const uint32_t at = lds_addr(ring + stage * T::STAGE);
+    return fetch_unit<DH, E4M3>(a, hk, t, len, page, at, at + 2 * T::BYTES, lane);
+  };
+  DecodeState<DH, E4M3> state;
+  state.clear();
+  uint32_t there = 0, next = 0;
+  if (wave < units) there = fetch(wave, 0);
+  const char* qrow = a.Q.p + b * a.Q.row + (int64_t)(head0 + min(q, heads - 1)) * a.Q.head;
+#pragma unroll
+  for (int s = 0; s < KS; ++s) state.qf[s] = *reinterpret_cast<const bf16x8*>(qrow + s * 64 + c * 16);
+#pragma unroll
+  for (int s = 0; s < KS; ++s) asm volatile("" ::"v"(state.qf[s]));   // (they are there: no wait for them in the loop)
+  for (int t = wave, stage = 0; t < units; t += WAVES, stage ^= 1, there = next) {
+    if (t + WAVES < units) {
+      next = fetch(t + WAVES, stage ^ 1);
+      wait_vmcnt<T::LOADS>();
+    } else {
+      wait_vmcnt<0>();
+    }
+    wave_lds_fence();
+    char* kt = ring + stage * T::STAGE;
+    state.unit(kt, kt + T::BYTES, kt + 2 * T::BYTES, there, a.cs, lane);
+    wave_lds_fence();
+    __builtin_amdgcn_s_waitcnt(0xC07F);                      // (lgkmcnt 0: the stage is filled again next)
+  }
+  const float sum = state.sum();
+  __syncthreads();
+  float* ml = reinterpret_cast<float*>(smem);                // [wave][16][2]
+  float* os = ml + WAVES * 32;                               // [wave][16][LD]
+  if (c == 0) {
+    ml[(wave * 16 + q) * 2] = state.m;
+    ml[(wave * 16 + q) * 2 + 1] = sum;
+  }
+#pragma unroll
+  for (int d = 0; d < DT; ++d) *reinterpret_cast<f32x4*>(os + (wave * 16 + q) * T::LD + 16 * d + 4 * c) = state.o[d];
+  __syncthreads();
+  for (int n = threadIdx.x; n < heads * (DH / 4); n += 64 * WAVES) {
+    const int row = n / (DH / 4), d4 = n % (DH / 4);
+    float M = -INFINITY, L = 0.f;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) M = fmaxf(M, ml[(w * 16 + row) * 2]);
+    const float ms = M == -INFINITY ? 0.f : M;
+    f32x4 y = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+      const float f = __builtin_amdgcn_exp2f(ml[(w * 16 + row) * 2] - ms);
+      const f32x4 x = *reinterpret_cast<const f32x4*>(os + (w * 16 + row) * T::LD + 4 * d4);
+      L = fmaf(f, ml[(w * 16 + row) * 2 + 1], L);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[e] = fmaf(f, x[e], y[e]);
+    }
+    const float inv = L == 0.f ? 0.f : 1.f / L;
+    *reinterpret_cast<uint2*>(a.Y.p + b * a.Y.row + (int64_t)(head0 + row) * a.Y.head + d4 * 8) =
+        make_uint2(pack_bf16x2(y[0] * inv, y[1] * inv), pack_bf16x2(y[2] * inv, y[3] * inv));
   }
 }
 
@@ -608,6 +715,25 @@ hipError_t launch_decode(DecodeTile<DH, E4M3, QC>, const DecodeArgs& a, hipStrea
   return hipGetLastError();
 }
 
+template <int DH, bool E4M3>
+hipError_t launch_items(const DecodeArgs& a, hipStream_t st) {
+  typedef ItemTile<DH, E4M3> T;
+  static std::atomic<uint64_t> done{0};
+  if (const hipError_t e = allow_smem(reinterpret_cast<const void*>(decode_item_kernel<DH, E4M3>), T::SMEM, done); e != hipSuccess) return e;
+  ScopedKernelTimer timer(kSlotAttnDecode, st);
+  hipLaunchKernelGGL((decode_item_kernel<DH, E4M3>), dim3(a.c.B * a.c.Hk * a.sets), dim3(64 * T::WAVES), T::SMEM, st, a);
+  return hipGetLastError();
+}
+
+// Whether a table is so narrow that a wavefront of an item's workgroup has four units at most: then the launch of the joins costs more than
+// an even split gains.  us a call in a graph, stretches and items, 32 heads on 8 of 128: 32 sequences of 512 tokens 19.2 and 14.2, one of
+// them 8.8 and 8.5, 64 of 10 to 1000 in 8 bits 16.6 and 15.7, 16 of 1000 14.4 and 12.2; one sequence of 100, 32 heads of 64: 8.4 and 4.2.
+// Wider tables: one of 1024 in 16 bits (four wavefronts) 9.3 and 13.4, one of 2048 in 8 bits 9.4 and 16.9.
+bool short_table(const spt_cache_shape_t& s) {
+  const int waves = s.format == SPT_CACHE_BF16 && s.dh == 128 ? ItemTile<128, false>::WAVES : ItemTile<64, false>::WAVES;
+  return (int64_t)s.max_pages * s.page <= 4 * kUnit * waves;
+}
+
 }  // namespace
 
 extern "C" int spt_cache_write(const spt_cache_shape_t* shape, int32_t T, const void* K, const void* V, const int64_t* strides,
@@ -675,6 +801,12 @@ extern "C" int spt_attn_decode(const spt_cache_shape_t* shape, int32_t H, float 
   a.workgroups = w.workgroups;
   a.cs = scale * kLog2e;
   const hipStream_t st = static_cast<hipStream_t>(stream);
+  if (short_table(s)) {
+    const bool e4m3 = s.format == SPT_CACHE_E4M3;
+    const hipError_t e = s.dh == 128 ? (e4m3 ? launch_items<128, true>(a, st) : launch_items<128, false>(a, st))
+                                     : (e4m3 ? launch_items<64, true>(a, st) : launch_items<64, false>(a, st));
+    return e == hipSuccess ? SPT_OK : SPT_ERR_HIP;
+  }
   const hipError_t e = with_tile(s, H, [&](auto t) { return launch_decode(t, a, st); });
   return e == hipSuccess ? SPT_OK : SPT_ERR_HIP;
 }

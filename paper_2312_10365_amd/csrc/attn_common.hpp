@@ -168,12 +168,9 @@ __device__ __forceinline__ uint32_t chunk_swizzle(int r) {
 template <int DH>
 __device__ __forceinline__ uint32_t row_swizzle(int r) { return chunk_swizzle<DH * 2>(r); }
 
-// Asynchronous copy global -> LDS, 16 (4) bytes per lane from base + off; lane L's data lands at lds_base + 16 L (4 L).
+// Asynchronous copy global -> LDS, 16 bytes per lane from base + off; lane L's data lands at lds_base + 16 L.
 __device__ __forceinline__ void dma16_at(const void* base, uint32_t off, uint32_t lds_base) {
   asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds_base), "v"(off), "s"(base) : "memory");
-}
-__device__ __forceinline__ void dma4_at(const void* base, uint32_t off, uint32_t lds_base) {
-  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds_base), "v"(off), "s"(base) : "memory");
 }
 __device__ __forceinline__ uint32_t lds_addr(const void* p) { return __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)p); }
 

@@ -83,6 +83,23 @@ def test_prompt(name):
     check_prompt(out, want_prompt(lens_q, lens_k, causal, Q, K, V, dY), sum(lens_q), sum(lens_k))
 
 
+LARGE = {   # more workgroups than are resident at once; gradients summed over many rows
+    "many_heads_64": ([333, 65, 0, 200, 500], [333, 65, 0, 200, 500], 64, 64, 64, True),
+    "many_heads_128": ([333, 65, 0, 200, 500], [333, 65, 0, 200, 500], 64, 16, 128, True),
+    "many_heads_full": ([300, 127, 640], [300, 127, 640], 32, 32, 64, False),
+    "many_heads_part": ([130, 257, 64], [700, 300, 1], 48, 16, 128, True),
+    "twelve_key_heads": ([400, 95, 33], [400, 95, 33], 24, 12, 128, True),
+}
+
+
+@pytest.mark.parametrize("name", LARGE)
+def test_prompt_large(name):
+    lens_q, lens_k, H, Hk, dh, causal = LARGE[name]
+    Q, K, V, dY = prompt_inputs(lens_q, lens_k, H, Hk, dh, seed=61)
+    out = run_prompt(lens_q, lens_k, causal, *(t.cuda() for t in (Q, K, V, dY)))
+    check_prompt(out, want_prompt(lens_q, lens_k, causal, Q, K, V, dY), sum(lens_q), sum(lens_k))
+
+
 @pytest.mark.parametrize("dh", [64, 128])
 @pytest.mark.parametrize("sharp,scale", [(12.0, None), (1.0, 1.0), (1.0, 1e-6)])
 def test_prompt_sharp_and_flat(dh, sharp, scale):
@@ -120,14 +137,15 @@ def test_prompt_views(dh):
 
 @pytest.mark.parametrize("dh", [64, 128])
 @pytest.mark.parametrize("value", [float("inf"), float("-inf"), float("nan")])
-def test_prompt_what_is_not_seen_does_not_matter(dh, value):
+@pytest.mark.parametrize("H,Hk", [(2, 1), (64, 64)])
+def test_prompt_what_is_not_seen_does_not_matter(dh, value, H, Hk):
     """A key (a query) that is not finite touches only the queries (the keys) of its own pairs."""
-    lens, H, Hk, at = [100, 90], 2, 1, 70
+    lens, at = [100, 90], 70
     Q, K, V, dY = prompt_inputs(lens, lens, H, Hk, dh, seed=21)
     clean = want_prompt(lens, lens, True, Q, K, V, dY)
     K2, V2 = K.clone(), V.clone()
-    K2[at, 0, 3] = value
-    V2[at, 0, 5] = value
+    K2[at, :, 3] = value
+    V2[at, :, 5] = value
     out = run_prompt(lens, lens, True, *(t.cuda() for t in (Q, K2, V2, dY)))
     other = np.r_[0:at, 100:190]                                  # queries in front of the key, and the other sequence
     for name in ("Y", "dQ"):
@@ -138,8 +156,8 @@ def test_prompt_what_is_not_seen_does_not_matter(dh, value):
         ref.check(name, ref.f64(out[name])[100:190], *(x[100:190] for x in clean[name]))
     # and a query: its gradients go to the keys that it sees
     Q2, dY2, q_at = Q.clone(), dY.clone(), 40
-    Q2[q_at, 0, 2] = value
-    dY2[q_at, 1, 7] = value
+    Q2[q_at, :, 2] = value
+    dY2[q_at, :, 7] = value
     out = run_prompt(lens, lens, True, *(t.cuda() for t in (Q2, K, V, dY2)))
     other = np.r_[q_at + 1:190]
     for name in ("dK", "dV"):
@@ -405,10 +423,12 @@ DECODES = {
 
 
 @pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("wide", [False, True])
 @pytest.mark.parametrize("name", DECODES)
-def test_decode(fmt, name):
+def test_decode(fmt, name, wide):
+    """Short sequences in a table made for them, and in one that could hold long ones."""
     lens, H, Hk, dh, page = DECODES[name]
-    shape, cache, table, Q, K, V = decode_inputs(fmt, lens, H, Hk, dh, page)
+    shape, cache, table, Q, K, V = decode_inputs(fmt, lens, H, Hk, dh, page, width=-(-max(max(lens), 3000) // page) if wide else None)
     Y = attn.decode(shape, Q.cuda(), cache, table, ints(lens))
     ref.check("Y", Y, *want_decode(Q, K, V, lens))
 
