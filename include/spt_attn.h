@@ -8,7 +8,9 @@
  * the host, enqueues on `stream` (a hipStream_t), never synchronises, never allocates; outputs are
  * overwritten; same inputs give bit-identical outputs (no floating-point atomics).  Return codes are
  * those of spt.h (SPT_OK, SPT_ERR_ARG, SPT_ERR_UNSUPPORTED, SPT_ERR_WORKSPACE, SPT_ERR_HIP).
- * Calls on several streams may overlap as long as they share no output and no workspace.
+ * Calls on several streams may overlap as long as they share no output and no workspace.  Outputs and workspaces share no
+ * memory with one another or with inputs.  What is not finite among the keys and values that a query sees makes what depends on
+ * it not finite; what it does not see does not matter.
  *
  * Heads: H query heads, Hk key heads, H % Hk == 0; query head h reads key head h / (H / Hk).
  * Head dimension dh: 64 or 128.
@@ -30,7 +32,7 @@ extern "C" {
 typedef struct {
   int32_t B;      /* sequences, 1 .. 4096; any of them may be empty */
   int32_t Tq, Tk; /* rows of Q, of K and V: at least one; cu_q[B] <= Tq, cu_k[B] <= Tk */
-  int32_t H, Hk;  /* query heads, key heads */
+  int32_t H, Hk;  /* query heads (at most 65535; B H and Tq H / 128 together below 2^23), key heads */
   int32_t dh;     /* 64 or 128 */
   int32_t causal; /* 0 or 1 */
   float scale;    /* logits are scale * q.k; positive and finite */
@@ -92,7 +94,7 @@ typedef struct {
  * entry of table outside 0 .. pages - 1, is not written; nothing else in the pool is touched.  Sequences that
  * share a page must not write the same token of it in one call.
  *   strides  host, or NULL for dense: elements per row and head of K, V: 4 numbers, as above
- *   table int32 [B][max_pages];  start int32 [B];  cu int32 [B+1] as above, cu[B] <= T */
+ *   table int32 [B][max_pages];  start int32 [B];  cu int32 [B+1] as above, cu[B] <= T;  T: 1 .. 2^26 - 1 */
 int spt_cache_write(const spt_cache_shape_t* shape, int32_t T, const void* K, const void* V, const int64_t* strides,
                     const int32_t* table, const int32_t* start, const int32_t* cu, void* Kc, void* Vc,
                     uint8_t* ks, uint8_t* vs, void* stream);
@@ -110,7 +112,7 @@ int spt_cache_read(const spt_cache_shape_t* shape, int32_t T, void* K, void* V, 
  *   Q, Y bf16 [B][H][dh];  strides host, or NULL for dense: of Q, Y: 4 numbers, as above
  *   lens int32 [B];  scale positive and finite
  *   ws: spt_attn_decode_workspace_bytes(shape, H) bytes, 256-byte aligned
- * B * Hk * ceil(max_pages * page / 32) * ceil(H / Hk / 16) must be below 2^31. */
+ * B * Hk * ceil(max_pages * page / 32) * ceil(H / Hk / 16) must be below 2^31, B * H below 2^23 - 16. */
 int spt_attn_decode(const spt_cache_shape_t* shape, int32_t H, float scale, const void* Q, const int64_t* strides,
                     const void* Kc, const void* Vc, const uint8_t* ks, const uint8_t* vs, const int32_t* table,
                     const int32_t* lens, void* Y, void* ws, size_t ws_bytes, void* stream);

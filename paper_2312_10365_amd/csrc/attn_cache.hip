@@ -187,7 +187,7 @@ __device__ __forceinline__ Line unit_line(const DecodeArgs& a) {
   for (int b = threadIdx.x & 63; b < a.c.B; b += 64) n += seq_units(a, b);
   n = wave_total(n) * a.c.Hk * a.sets;
   const int waves = a.workgroups * kDecodeWaves;
-  return {n, max(kLeastUnits, (n + waves - 1) / waves)};
+  return {n, max(kLeastUnits, (n - 1) / waves + 1)};
 }
 // First unit of sequence b's items
 __device__ __forceinline__ int units_before(const DecodeArgs& a, int b) {
@@ -657,11 +657,14 @@ CacheArgs cache_args(const spt_cache_shape_t& s, const void* Kc, const void* Vc,
           const_cast<uint8_t*>(vs), table, s.pages, __builtin_ctz(s.page), s.Hk, s.B, s.max_pages};
 }
 
+constexpr int kMostRows = (1 << 26) - 1;   // (a wavefront each)
+
 int check_rows(const spt_cache_shape_t* s, int32_t T, const void* K, const void* V, const int64_t* strides, const int32_t* start, const int32_t* cu,
                bool output, RowArgs* a) {
   int rc = check_cache(s);
   if (rc != SPT_OK) return rc;
   if (T < 1) return SPT_ERR_ARG;
+  if (T > kMostRows) return SPT_ERR_UNSUPPORTED;
   if ((rc = attn_rows(&a->K, K, strides, T, s->Hk, s->dh, output)) != SPT_OK) return rc;
   if ((rc = attn_rows(&a->V, V, strides ? strides + 2 : nullptr, T, s->Hk, s->dh, output)) != SPT_OK) return rc;
   if (!aligned_to(start, 4) || !aligned_to(cu, 4)) return SPT_ERR_ARG;
@@ -696,7 +699,7 @@ int check_decode(const spt_cache_shape_t* s, int32_t H) {
   if (H < 1 || H % s->Hk != 0) return SPT_ERR_ARG;
   if (H > 65535) return SPT_ERR_UNSUPPORTED;
   const int64_t units = ((int64_t)s->max_pages * s->page + kUnit - 1) / kUnit * s->Hk * ((H / s->Hk + 15) / 16);
-  if (units > INT_MAX || units * s->B > INT_MAX || (int64_t)s->B * H > INT_MAX) return SPT_ERR_UNSUPPORTED;
+  if (units > INT_MAX || units * s->B > INT_MAX || (int64_t)s->B * H > kMostWorkgroups) return SPT_ERR_UNSUPPORTED;
   return SPT_OK;
 }
 

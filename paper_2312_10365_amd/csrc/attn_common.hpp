@@ -48,6 +48,8 @@ inline hipError_t allow_smem(const void* kernel, int smem, std::atomic<uint64_t>
   return e;
 }
 
+constexpr int64_t kMostWorkgroups = (1 << 23) - 16;   // of up to 512 threads: a launch has fewer than 2^32
+
 int check_attn(const spt_attn_shape_t* s);   // attn_prompt.hip
 int attn_heads_shift(int G);                // log2 of the heads of a group of G that share a workgroup
 

@@ -269,8 +269,9 @@ int check_attn(const spt_attn_shape_t* s) {
   if (s->causal != 0 && s->causal != 1) return SPT_ERR_ARG;
   if (!isfinite(s->scale) || !(s->scale > 0.f)) return SPT_ERR_ARG;
   if ((s->dh != 64 && s->dh != 128) || s->B > 4096 || s->H > 65535) return SPT_ERR_UNSUPPORTED;
-  // (workgroups: tiles of 32 rows at least, in every sequence, times heads, and a few)
-  if (((int64_t)s->Tq / 32 + s->B) * s->H > INT_MAX - 8 || ((int64_t)s->Tk / 32 + s->B) * s->H > INT_MAX - 8) return SPT_ERR_UNSUPPORTED;
+  const int shift = attn_heads_shift(s->H / s->Hk);   // (tiles of 128 rows of heads; of 128 keys)
+  if (((int64_t)(s->Tq >> (7 - shift)) + s->B) * (s->H >> shift) > kMostWorkgroups) return SPT_ERR_UNSUPPORTED;
+  if (((int64_t)(s->Tk >> 7) + s->B) * s->Hk > kMostWorkgroups) return SPT_ERR_UNSUPPORTED;
   return SPT_OK;
 }
 

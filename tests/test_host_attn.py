@@ -130,6 +130,20 @@ def test_decode_arguments():
     assert 0 < small < large
 
 
+def test_no_launch_of_2_to_32_threads():
+    """A launch counts its threads in 32 bits: refused on the host, workspace sizes included."""
+    s = pool(dict(B=65535))
+    assert attn.decode_workspace_bytes(s, 128) > 0
+    assert decode(s, H=130) == UNSUPPORTED and attn.decode_workspace_bytes(s, 130) == 0
+    for read in (False, True):
+        assert write(pool(), T=1 << 26, read=read) == UNSUPPORTED and write(pool(), T=2 ** 31 - 1, read=read) == UNSUPPORTED
+    assert attn.prompt_workspace_bytes(attn.make_shape(4096, 1 << 20, 1 << 20, 128, 8, 64)) > 0
+    for n in (dict(B=4096, Tq=1, Tk=1, H=2048, Hk=2048), dict(B=1, Tq=2 ** 31 - 1, Tk=1, H=1, Hk=1), dict(B=1, Tq=1, Tk=1 << 30, H=1, Hk=1),
+              dict(B=1, Tq=1 << 28, Tk=1, H=4, Hk=1)):
+        shape = attn.make_shape(dh=64, **n)
+        assert fwd(shape) == UNSUPPORTED and bwd(shape) == UNSUPPORTED and attn.prompt_workspace_bytes(shape) == 0, n
+
+
 def test_binding_refuses_before_it_calls():
     s = attn.make_shape(1, 4, 4, 2, 1, 64)
     q, k = ref.bf16(4, 2, 64, seed=1), ref.bf16(4, 1, 64, seed=2)
