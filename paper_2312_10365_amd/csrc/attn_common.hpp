@@ -53,6 +53,16 @@ constexpr int64_t kMostWorkgroups = (1 << 23) - 16;   // of up to 512 threads: a
 int check_attn(const spt_attn_shape_t* s);   // attn_prompt.hip
 int attn_heads_shift(int G);                // log2 of the heads of a group of G that share a workgroup
 
+// How coarsely find_tile orders tiles by their work, as a power of two: as many tiles as there are rounds of resident workgroups.  Strictly
+// by work, tiles that read the same rows are as far apart as there are sequences, and L2 does not hold what lies between; in few rounds the
+// order matters more.  us of the forward with `causal`, by work alone, so, and sequence by sequence: 32 heads of 128, 48 sequences of
+// 512 (12 rounds) 280, 196, 197; 32 of 33 to 2000 424, 380, 370; 32 heads on 8, 48 of 33 to 2000 563, 524, 514; 32 heads of 64,
+// 64 of 512 173, 142, 141, 8 of them (one round) 23.2, 23.3, 28.5.
+inline int coarse_tiles(int64_t workgroups, int on_a_cu) {
+  const int64_t rounds = workgroups / (256 * on_a_cu);
+  return rounds < 1 ? 0 : 63 - __builtin_clzll(rounds);
+}
+
 // ---- device side
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
@@ -82,52 +92,38 @@ __device__ __forceinline__ int wave_prefix(int x) {
 }
 __device__ __forceinline__ int wave_total(int x) { return __builtin_amdgcn_readlane(wave_prefix(x), 63); }
 
-// A workgroup's row tile: its sequence, the tile's number in it, and the sequence's rows in both tensors.
+// A workgroup's row tile: its number in its sequence, and the sequence's rows in both tensors.
 struct TilePlace {
-  int b, tile;
+  int tile;
   SeqRows own, other;
 };
 
-// Tile t in the order in which workgroups take them.  All lanes of a wavefront look together.  Up to 64 sequences: the tiles
+// Tile t in the order in which workgroups take them.  All lanes of a wavefront look together.  64 sequences at a time: the tiles
 // with the most work first, whatever their sequence (work in tiles of the other side: with `causal` tile k of queries has k and the
-// keys that were there before, tile k of keys, FROM_END, what is left behind it; without, every tile all rows of the other side).  More:
-// sequence by sequence, with `causal` from the tile with the most work on.
+// keys that were there before, tile k of keys, FROM_END, what is left behind it; without, every tile all rows of the other side).  With `causal`
+// 1 << coarse tiles of work count as the same, and those of a sequence come one after the other.
 template <bool FROM_END>
 __device__ __forceinline__ bool find_tile(const int32_t* cu_own, const int32_t* cu_other, int B, int Town, int Tother, int shift, bool causal,
-                                          int t, TilePlace& p) {
+                                          int coarse, int t, TilePlace& p) {
   const int lane = threadIdx.x & 63, round = (1 << shift) - 1;
-  if (B > 64) {
-    int before = 0;
-    for (int b0 = 0; b0 < B; b0 += 64) {
-      const int n = b0 + lane < B ? (seq_rows(cu_own, b0 + lane, Town).n + round) >> shift : 0;
-      const int incl = wave_prefix(n), total = __builtin_amdgcn_readlane(incl, 63);
-      if (t - before < total) {
-        const int src = __builtin_ctzll(__ballot(incl > t - before));
-        const int k = t - before - (src > 0 ? __builtin_amdgcn_readlane(incl, src - 1) : 0);
-        p.b = b0 + src;
-        p.tile = FROM_END ? k : __builtin_amdgcn_readlane(n, src) - 1 - k;
-        p.own = seq_rows(cu_own, p.b, Town);
-        p.other = seq_rows(cu_other, p.b, Tother);
-        return true;
-      }
-      before += total;
-    }
-    return false;
-  }
   SeqRows own = {0, 0}, other = {0, 0};
-  if (lane < B) {
-    own = seq_rows(cu_own, lane, Town);
-    other = seq_rows(cu_other, lane, Tother);
+  int n, total;                                            // tiles of the lane's sequence, of 64
+  for (int b0 = 0;; b0 += 64, t -= total) {
+    if (b0 >= B) return false;
+    own = b0 + lane < B ? seq_rows(cu_own, b0 + lane, Town) : SeqRows{0, 0};
+    n = (own.n + round) >> shift;
+    total = wave_total(n);
+    if (t < total) {
+      if (b0 + lane < B) other = seq_rows(cu_other, b0 + lane, Tother);
+      break;
+    }
   }
-  const int n = (own.n + round) >> shift;
   const int base = !causal ? other.n >> shift : FROM_END ? 0 : max(0, other.n - own.n) >> shift;
-  // tiles of the lane's sequence with work of at least x + 1
-  auto count = [&](int x) { return causal ? min(max(base + n - x, 0), n) : base >= x ? n : 0; };
-  int lo = 0, hi = 1, above = 0;                           // total(lo) > t >= total(hi)
-  if (wave_total(n) <= t) return false;
+  // tiles of the lane's sequence with work of at least x + 1 steps
+  auto count = [&](int x) { return causal ? min(max(base + n - (x << coarse), 0), n) : base >= x ? n : 0; };
+  int lo = 0, hi = 1, b = 0;                               // total(lo) > t >= total(hi)
   if (B == 1) {
     p.tile = causal ? __builtin_amdgcn_readfirstlane(n) - 1 - t : t;
-    p.b = 0;
   } else {
     for (; wave_total(count(hi)) > t; hi *= 2) lo = hi;
     while (hi - lo > 1) {
@@ -135,14 +131,15 @@ __device__ __forceinline__ bool find_tile(const int32_t* cu_own, const int32_t* 
       if (wave_total(count(mid)) > t) lo = mid;
       else hi = mid;
     }
-    above = wave_total(count(hi));
-    const int incl = wave_prefix(count(lo) - count(hi));
-    p.b = __builtin_ctzll(__ballot(incl > t - above));
-    p.tile = causal ? lo - __builtin_amdgcn_readlane(base, p.b) : t - above - (p.b > 0 ? __builtin_amdgcn_readlane(incl, p.b - 1) : 0);
+    const int more = count(hi), incl = wave_prefix(count(lo) - more);
+    t -= wave_total(more);
+    b = __builtin_ctzll(__ballot(incl > t));
+    if (b > 0) t -= __builtin_amdgcn_readlane(incl, b - 1);
+    p.tile = causal ? __builtin_amdgcn_readlane(n - more, b) - 1 - t : t;
   }
-  if (FROM_END && causal) p.tile = __builtin_amdgcn_readlane(n, p.b) - 1 - p.tile;
-  p.own = {__builtin_amdgcn_readlane(own.first, p.b), __builtin_amdgcn_readlane(own.n, p.b)};
-  p.other = {__builtin_amdgcn_readlane(other.first, p.b), __builtin_amdgcn_readlane(other.n, p.b)};
+  if (FROM_END && causal) p.tile = __builtin_amdgcn_readlane(n, b) - 1 - p.tile;
+  p.own = {__builtin_amdgcn_readlane(own.first, b), __builtin_amdgcn_readlane(own.n, b)};
+  p.other = {__builtin_amdgcn_readlane(other.first, b), __builtin_amdgcn_readlane(other.n, b)};
   return true;
 }
 

@@ -21,7 +21,7 @@ struct FwdArgs {
   const int32_t *cu_q, *cu_k;
   float* lse;
   int B, Tq, Tk, Hk, G, hshift;   // G = H / Hk, 1 << hshift heads of a group in a workgroup
-  int causal;
+  int causal, coarse;
   float c;
 };
 
@@ -66,7 +66,7 @@ __global__ __launch_bounds__(256 * GROUPS, 2) void prompt_fwd_kernel(const FwdAr
   const HeadItem w = head_item(blockIdx.x, a.Hk);
   const int hk = w.hk, hs = w.item % hsets;
   TilePlace at;
-  if (!find_tile<false>(a.cu_q, a.cu_k, a.B, a.Tq, a.Tk, pshift, a.causal, w.item / hsets, at)) return;
+  if (!find_tile<false>(a.cu_q, a.cu_k, a.B, a.Tq, a.Tk, pshift, a.causal, a.coarse, w.item / hsets, at)) return;
   const int tile = at.tile;
   const SeqRows sq = at.own, sk = at.other;
   const int nq = sq.n, nk = sk.n, ahead = nk - nq;       // query i sees keys up to i + ahead
@@ -297,6 +297,7 @@ extern "C" int spt_attn_prompt_fwd(const spt_attn_shape_t* shape, const void* Q,
   a.hshift = attn_heads_shift(a.G);
   const int grid = head_item_grid(s.Hk, ((s.Tq >> (7 - a.hshift)) + s.B) * (a.G >> a.hshift));   // (tiles: so many at most)
   a.causal = s.causal;
+  a.coarse = coarse_tiles((int64_t)(s.Tq >> (7 - a.hshift)) * (s.H >> a.hshift), s.dh == 128 ? 2 : 4);
   a.c = s.scale * kLog2e;
   const hipStream_t st = static_cast<hipStream_t>(stream);
   ScopedKernelTimer timer(kSlotAttnFwd, st);

@@ -26,7 +26,7 @@ struct BwdArgs {
   const float* lse;
   float *off, *neg_d;             // [H][Tq]: row_offset(lse), -D
   int B, Tq, Tk, Hk, G, hshift;
-  int causal;
+  int causal, coarse;
   float c, scale;
 };
 
@@ -100,7 +100,7 @@ __global__ __launch_bounds__(256, 2) void prompt_bwd_q_kernel(const BwdArgs a) {
   const HeadItem w = head_item(blockIdx.x, a.Hk);
   const int hk = w.hk, hs = w.item % hsets;
   TilePlace at;
-  if (!find_tile<false>(a.cu_q, a.cu_k, a.B, a.Tq, a.Tk, pshift, a.causal, w.item / hsets, at)) return;
+  if (!find_tile<false>(a.cu_q, a.cu_k, a.B, a.Tq, a.Tk, pshift, a.causal, a.coarse, w.item / hsets, at)) return;
   const int tile = at.tile;
   const SeqRows sq = at.own, sk = at.other;
   const int nq = sq.n, nk = sk.n, ahead = nk - nq;
@@ -305,7 +305,7 @@ __global__ __launch_bounds__(256 * GROUPS, 2) void prompt_bwd_kv_kernel(const Bw
   const HeadItem w = head_item(blockIdx.x, a.Hk);
   const int hk = w.hk;
   TilePlace place;
-  if (!find_tile<true>(a.cu_k, a.cu_q, a.B, a.Tk, a.Tq, 7, a.causal, w.item, place)) return;
+  if (!find_tile<true>(a.cu_k, a.cu_q, a.B, a.Tk, a.Tq, 7, a.causal, a.coarse, w.item, place)) return;
   const int tile = place.tile;
   const SeqRows sk = place.own, sq = place.other;
   const int nq = sq.n, nk = sk.n, ahead = nk - nq;
@@ -573,6 +573,7 @@ extern "C" int spt_attn_prompt_bwd(const spt_attn_shape_t* shape, const void* Q,
   const hipStream_t st = static_cast<hipStream_t>(stream);
   {
     ScopedKernelTimer timer(kSlotAttnBwdQ, st);
+    a.coarse = coarse_tiles((int64_t)(s.Tq >> (7 - a.hshift)) * (s.H >> a.hshift), s.dh == 128 ? 2 : 3);
     const int grid = head_item_grid(s.Hk, ((s.Tq >> (7 - a.hshift)) + s.B) * (a.G >> a.hshift));
     const auto kernel = s.dh == 128 ? (few ? prompt_bwd_q_kernel<128, true> : prompt_bwd_q_kernel<128, false>)
                                     : (few ? prompt_bwd_q_kernel<64, true> : prompt_bwd_q_kernel<64, false>);
@@ -580,6 +581,9 @@ extern "C" int spt_attn_prompt_bwd(const spt_attn_shape_t* shape, const void* Q,
     if (hipGetLastError() != hipSuccess) return SPT_ERR_HIP;
   }
   ScopedKernelTimer timer(kSlotAttnBwdKV, st);
+  // (heads that share their keys make fewer and longer tiles, of which the order by work alone is better: us, 48 sequences of 512, 32 heads of
+  // 128 on 8 318 and 410 so, on 16 385 and 381, on 32 496 and 445)
+  a.coarse = a.G > 1 ? 0 : coarse_tiles((int64_t)(s.Tk / kOwnKeys) * s.Hk, s.dh == 128 ? 1 : 3);
   const int grid = head_item_grid(s.Hk, s.Tk / kOwnKeys + s.B);
   const hipError_t e = s.dh == 128 ? (few ? launch_kv<128, 2, true>(a, grid, st) : launch_kv<128, 2, false>(a, grid, st))
                                    : (few ? launch_kv<64, 1, true>(a, grid, st) : launch_kv<64, 1, false>(a, grid, st));

@@ -89,6 +89,9 @@ LARGE = {   # more workgroups than are resident at once; gradients summed over m
     "many_heads_full": ([300, 127, 640], [300, 127, 640], 32, 32, 64, False),
     "many_heads_part": ([130, 257, 64], [700, 300, 1], 48, 16, 128, True),
     "twelve_key_heads": ([400, 95, 33], [400, 95, 33], 24, 12, 128, True),
+    "rounds_64": ([333, 65, 0, 200, 500], [333, 65, 0, 200, 500], 256, 256, 64, True),
+    "rounds_128": ([300, 0, 200, 77], [300, 0, 410, 77], 256, 256, 128, True),
+    "many_sequences": ([(7 * i) % 61 for i in range(150)], [(7 * i) % 61 + (5 * i) % 23 for i in range(150)], 128, 64, 64, True),
 }
 
 
