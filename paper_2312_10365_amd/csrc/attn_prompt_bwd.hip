@@ -214,6 +214,7 @@ __global__ __launch_bounds__(256, 2) void prompt_bwd_q_kernel(const BwdArgs a) {
     }
     if (j0 >= wave_kend) continue;
     const bool masked = j0 + kTile > wave_full;
+    __builtin_amdgcn_iglp_opt(1);                        // (reads of LDS between the products: see the forward)
     f32x16 s, dp;
     first_products(t, s, dp);
     second_products(t, weights(t, s, dp, masked));
@@ -453,9 +454,11 @@ __global__ __launch_bounds__(256 * GROUPS, 2) void prompt_bwd_kv_kernel(const Bw
       for (int u = 0; u < 2 * TILE_BYTES / 4096; ++u) not_finite.look(lds_read<u32x4>(tiles + buf * 2 * TILE_BYTES + u * 4096 + tid * 16));
     }
     if (q0 < wave_begin) continue;
+    const bool cut = masked && ((a.causal && q0 < j0 + 31 - ahead) || q0 + kTile > nq);   // (some query of the tile does not see some key of the wavefront)
+    __builtin_amdgcn_iglp_opt(1);                                        // (reads of LDS between the products: see the forward)
     f32x16 s, dp;
     first_products(buf, s, dp);
-    second_products(buf, weights(buf, q0, s, dp, masked));
+    second_products(buf, weights(buf, q0, s, dp, cut));
   }
   // rows that not all keys may see hold infinities or NaN: 0 times those is NaN
   if (masked_steps > 0 && __syncthreads_or(not_finite.found())) {
