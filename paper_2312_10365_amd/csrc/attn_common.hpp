@@ -63,6 +63,15 @@ inline int coarse_tiles(int64_t workgroups, int on_a_cu) {
   return rounds < 1 ? 0 : 63 - __builtin_clzll(rounds);
 }
 
+// Whether the 128 rows of a workgroup are dealt to four, whose wavefronts share what passes through LDS (`through` rows of B sequences)
+// instead of owning 32 rows each: where the four fit onto the chip at once and there is enough to share.  us, 128 rows and 32.
+// Forward: 8 heads of 128, 256 tokens 10.8 and 10.3, 512 14.3 and 12.1; 24 heads of 64, 384 (72 workgroups) 10.6 and 14.2; 2 heads, 4000 42 and 23.
+// Query side of the gradients: 12 heads of 64, 160 11.5 and 12.2, 256 14.1 and 12.6, 512 20.7 and 14.0; 24 heads, 384 15.7 and 20.6;
+// 2 heads, 4000 106 and 32.  Key side: 12 heads of 64, 77 10.5 and 11.8, 160 13.4 and 12.1, 512 24.5 and 14.3; 24 heads, 384
+// 18.2 and 20.3; 32 heads of 64 on 8, 512 61 and 23, of 128 on 8 63 and 37, 1024 115 and 64.
+constexpr int kFewTiles = 64;
+inline bool split_rows(int64_t workgroups, int64_t through, int B) { return workgroups <= kFewTiles && through >= 192 * (int64_t)B; }
+
 // ---- device side
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;

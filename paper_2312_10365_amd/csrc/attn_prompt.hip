@@ -1,19 +1,21 @@
 // Full attention over packed sequences, forward (include/spt_attn.h).
 //
 // A workgroup of four wavefronts owns 128 query rows: 128 / HW positions of one sequence times HW heads that
-// share a key head (HW: 4, 2 or 1, as divides the group).  A wavefront owns 32 of them.  Keys and values pass through LDS in
-// tiles of 64, copied asynchronously one tile ahead.  Scores are formed transposed, S^T = K Q^T, so that a lane holds 16
+// share a key head (HW: 4, 2 or 1, as divides the group).  A wavefront owns 32 of them.  Where there is less to do than the chip has
+// room for, two such groups share the keys, or four or eight wavefronts the keys of 32 rows.  Keys and values pass through LDS in
+// tiles of 64 (32 so), copied asynchronously one tile ahead.  Scores are formed transposed, S^T = K Q^T, so that a lane holds 16
 // scores of ONE query and half of them are what the second product's operand wants of it: P stays in registers, and
 // maximum, sum and rescaling of a query are one lane's (two halves of a row meet in one lane swap).  O^T = V^T P^T takes V out of LDS
 // through the transposing read.  One pass over the keys: running maximum m and sum l, p = 2^(c s - m) with c = scale log2 e; the
 // accumulators are rescaled only when a maximum rises by more than 2^8 (p stays below 256, and the sums are fp32).
+#include <type_traits>
+
 #include "attn_common.hpp"
 
 using namespace spt;
 
 namespace {
 
-constexpr int kTileKeys = 64;
 constexpr float kLazy = 8.f;   // a row's maximum may be this much (log2) above what its sums are scaled by
 
 struct FwdArgs {
@@ -53,16 +55,25 @@ __device__ __forceinline__ void slow_row(const char* q, const char* k, int64_t k
   if (lse && lane == 0) *lse = (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
-// GROUPS: groups of four wavefronts that go through every GROUPS-th tile of keys for the same queries.
-template <int DH, int GROUPS>
-__global__ __launch_bounds__(256 * GROUPS, 2) void prompt_fwd_kernel(const FwdArgs a) {
-  constexpr int KS = DH / 16, DT = DH / 32, TILE_BYTES = kTileKeys * DH * 2, RING = 4 * TILE_BYTES;   // K, V, twice
-  extern __shared__ __align__(256) char smem[];
-  const int lane = threadIdx.x & 63, i = lane & 31, h = lane >> 5, tid = threadIdx.x & 255;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) & 3, group = GROUPS == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 8);
-  char* ring = smem + group * RING;
+// A workgroup: GROUPS groups of OWNERS wavefronts (four or one), which go through every GROUPS-th tile of 32 KT keys for the same queries.
+template <int DH, int OWNERS, int GROUPS>
+struct FwdSizes {
+  static constexpr int KT = OWNERS == 4 ? 2 : 1, TILE_KEYS = 32 * KT, TILE_BYTES = TILE_KEYS * DH * 2, RING = 4 * TILE_BYTES;   // K, V, twice
+  static constexpr int SHIFT = OWNERS == 4 ? 7 : 5, PART = DH * 128 + 512;   // 1 << SHIFT: rows; a wavefront's sums
+  static constexpr int RINGS = GROUPS * RING, PARTS = (GROUPS - 1) * OWNERS * PART, SMEM = RINGS > PARTS ? RINGS : PARTS;
+  static_assert(SMEM <= 160 * 1024, "a CU's LDS");
+};
 
-  const int hsets = a.G >> a.hshift, pshift = 7 - a.hshift;               // 1 << pshift positions of a workgroup
+template <int DH, int OWNERS, int GROUPS>
+__global__ __launch_bounds__((64 * OWNERS * GROUPS), 2) void prompt_fwd_kernel(const FwdArgs a) {
+  typedef FwdSizes<DH, OWNERS, GROUPS> Sizes;
+  constexpr int KS = DH / 16, DT = DH / 32, KT = Sizes::KT, TILE_KEYS = Sizes::TILE_KEYS, TILE_BYTES = Sizes::TILE_BYTES;
+  extern __shared__ __align__(256) char smem[];
+  const int lane = threadIdx.x & 63, i = lane & 31, h = lane >> 5, tid = threadIdx.x % (64 * OWNERS);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % OWNERS, group = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) / OWNERS;
+  char* ring = smem + group * Sizes::RING;
+
+  const int hsets = a.G >> a.hshift, pshift = Sizes::SHIFT - a.hshift;    // 1 << pshift positions of a workgroup
   const HeadItem w = head_item(blockIdx.x, a.Hk);
   const int hk = w.hk, hs = w.item % hsets;
   TilePlace at;
@@ -78,7 +89,7 @@ __global__ __launch_bounds__(256 * GROUPS, 2) void prompt_fwd_kernel(const FwdAr
   const int wave_full = i0 >= nq ? 0 : a.causal ? min(nk, i0 + ahead + 1) : nk;   // ... that all queries of the wavefront see
   const int mine = min(i0 + i, nq - 1);
   const int seen = a.causal ? min(nk, mine + ahead + 1) : nk;            // keys the lane's query sees (may be negative)
-  const int ntile = kend > 0 ? (kend + kTileKeys - 1) / kTileKeys : 0;
+  const int ntile = kend > 0 ? (kend + TILE_KEYS - 1) / TILE_KEYS : 0;
   const int full = max(0, a.causal ? min(nk, p0 + ahead + 1) : nk);     // keys that all queries of the workgroup see
 
   // the wavefront's queries, through the second ring buffer: whole lines
@@ -87,18 +98,18 @@ __global__ __launch_bounds__(256 * GROUPS, 2) void prompt_fwd_kernel(const FwdAr
   fetch_rows<DH>(qbase + min(i0, nq - 1) * a.Q.row, a.Q.row, max(nq - i0, 1), tiles + mine_lds, lane);
   const char* kbase = a.K.p + (int64_t)sk.first * a.K.row + (int64_t)hk * a.K.head;
   const char* vbase = a.V.p + (int64_t)sk.first * a.V.row + (int64_t)hk * a.V.head;
-  // copies: lane L of an instruction fills 16 bytes of row (u 256 + tid) / (DH / 8)
-  constexpr int COPIES = kTileKeys * (DH / 8) / 256;
+  // copies: lane L of an instruction fills 16 bytes of row (u 64 OWNERS + tid) / (DH / 8)
+  constexpr int COPIES = TILE_KEYS * (DH / 8) / (64 * OWNERS);
   auto fetch = [&](int t, int buf) {
-    const int j0 = t * kTileKeys;
+    const int j0 = t * TILE_KEYS;
     const char* kb = kbase + (int64_t)j0 * a.K.row;
     const char* vb = vbase + (int64_t)j0 * a.V.row;
 #pragma unroll
     for (int u = 0; u < COPIES; ++u) {
-      const int slot = u * 256 + tid, row = slot / (DH / 8);
+      const int slot = u * 64 * OWNERS + tid, row = slot / (DH / 8);
       const uint32_t chunk = ((slot % (DH / 8)) ^ row_swizzle<DH>(row)) * 16;
       const uint32_t r = (uint32_t)min(row, nk - 1 - j0);               // (rows past the end: the last one again)
-      const uint32_t at = lds_addr(ring + buf * 2 * TILE_BYTES + u * 4096 + wave * 1024);
+      const uint32_t at = lds_addr(ring + buf * 2 * TILE_BYTES + (u * OWNERS + wave) * 1024);
       dma16_at(kb, r * (uint32_t)a.K.row + chunk, at);
       dma16_at(vb, r * (uint32_t)a.V.row + chunk, at + TILE_BYTES);
     }
@@ -121,36 +132,36 @@ __global__ __launch_bounds__(256 * GROUPS, 2) void prompt_fwd_kernel(const FwdAr
   for (int t0 = 0; t0 < ntile; t0 += GROUPS) {
     wait_vmcnt<0>();
     __syncthreads();
-    const int t = t0 + group, buf = t0 / GROUPS & 1, j0 = t * kTileKeys;
+    const int t = t0 + group, buf = t0 / GROUPS & 1, j0 = t * TILE_KEYS;
     if (t + GROUPS < ntile) fetch(t + GROUPS, buf ^ 1);
     if (t >= ntile) continue;
     const uint32_t kt_ = tiles + buf * 2 * TILE_BYTES, vt_ = kt_ + TILE_BYTES;
-    if (j0 + kTileKeys > full) {
+    if (j0 + TILE_KEYS > full) {
 #pragma unroll
-      for (int u = 0; u < TILE_BYTES / 4096; ++u) not_finite.look(lds_read<u32x4>(vt_ + u * 4096 + tid * 16));
+      for (int u = 0; u < TILE_BYTES / (1024 * OWNERS); ++u) not_finite.look(lds_read<u32x4>(vt_ + u * 1024 * OWNERS + tid * 16));
     }
     if (j0 >= wave_kend) continue;
     lds.fresh();
     __builtin_amdgcn_iglp_opt(1);                        // the compiler deals reads of LDS out between products: 8192 tokens, 32 heads of 128 on 8, 535 us without, 521
-    f32x16 s[2];
+    f32x16 s[KT];
 #pragma unroll
-    for (int kt = 0; kt < 2; ++kt) {
+    for (int kt = 0; kt < KT; ++kt) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) s[kt][r] = 0.f;
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks)
         s[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lds.rows(kt_, kt, ks), qf[ks], s[kt], 0, 0, 0);
     }
-    if (j0 + kTileKeys > wave_full) {
+    if (j0 + TILE_KEYS > wave_full) {
       const int left = seen - j0 - 4 * h;
 #pragma unroll
-      for (int kt = 0; kt < 2; ++kt)
+      for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
         for (int r = 0; r < 16; ++r) s[kt][r] = 32 * kt + 8 * (r >> 2) + (r & 3) < left ? s[kt][r] : -INFINITY;
     }
     float top = s[0][0];
 #pragma unroll
-    for (int r = 1; r < 32; ++r) top = fmaxf(top, s[r >> 4][r & 15]);
+    for (int r = 1; r < 16 * KT; ++r) top = fmaxf(top, s[r >> 4][r & 15]);
     top = fmaxf(top, other_half(top)) * a.c;
     if (__any(top > m + kLazy)) {
       const float mn = fmaxf(m, top), ms = mn == -INFINITY ? 0.f : mn;
@@ -163,9 +174,9 @@ __global__ __launch_bounds__(256 * GROUPS, 2) void prompt_fwd_kernel(const FwdAr
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[d][r] *= alpha;
     }
-    bf16x8 pf[2][2];
+    bf16x8 pf[KT][2];
 #pragma unroll
-    for (int kt = 0; kt < 2; ++kt)
+    for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
         float p[8];
@@ -177,7 +188,7 @@ __global__ __launch_bounds__(256 * GROUPS, 2) void prompt_fwd_kernel(const FwdAr
         pf[kt][half] = pack8(p);
       }
 #pragma unroll
-    for (int kt = 0; kt < 2; ++kt)
+    for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
       for (int half = 0; half < 2; ++half)
 #pragma unroll
@@ -187,7 +198,7 @@ __global__ __launch_bounds__(256 * GROUPS, 2) void prompt_fwd_kernel(const FwdAr
 
   float* lse = a.lse ? a.lse + (int64_t)head * a.Tq + sq.first : nullptr;
   // rows of V that not all queries may see hold infinities or NaN: 0 times those is NaN
-  if (full < ntile * kTileKeys && __syncthreads_or(not_finite.found())) {
+  if (full < ntile * TILE_KEYS && __syncthreads_or(not_finite.found())) {
     for (int r = group; r < min(32, nq - i0); r += GROUPS) {
       const int row = i0 + r;
       slow_row<DH>(a.Q.p + (int64_t)(sq.first + row) * a.Q.row + (int64_t)head * a.Q.head, kbase, a.K.row, vbase, a.V.row,
@@ -197,39 +208,43 @@ __global__ __launch_bounds__(256 * GROUPS, 2) void prompt_fwd_kernel(const FwdAr
     return;
   }
   l += other_half(l);
-  if (GROUPS == 2) {                                     // the second group's part, scaled to the larger maximum of the two
-    float* part = reinterpret_cast<float*>(smem) + wave * (DT * 1024 + 128) + lane * 4;
-    float* ml = reinterpret_cast<float*>(smem) + wave * (DT * 1024 + 128) + DT * 1024;
+  if (GROUPS > 1) {                                      // the other groups' parts in order, scaled to the larger maximum
+    auto part = [&](int g) { return reinterpret_cast<float*>(smem + ((g - 1) * OWNERS + wave) * Sizes::PART); };
     __syncthreads();
-    if (group == 1) {
+    if (group > 0) {
+      float *x = part(group) + lane * 4, *ml = part(group) + DT * 1024 + lane;
 #pragma unroll
       for (int d = 0; d < DT; ++d)
 #pragma unroll
-        for (int q = 0; q < 4; ++q) *reinterpret_cast<f32x4*>(part + (d * 4 + q) * 256) = f32x4{o[d][4 * q], o[d][4 * q + 1], o[d][4 * q + 2], o[d][4 * q + 3]};
-      ml[lane] = m;
-      ml[64 + lane] = l;
+        for (int q = 0; q < 4; ++q) *reinterpret_cast<f32x4*>(x + (d * 4 + q) * 256) = f32x4{o[d][4 * q], o[d][4 * q + 1], o[d][4 * q + 2], o[d][4 * q + 3]};
+      ml[0] = m;
+      ml[64] = l;
     }
     __syncthreads();
-    if (group == 1) return;
-    const float m1 = ml[lane], mn = fmaxf(m, m1), ms = mn == -INFINITY ? 0.f : mn;
-    const float f0 = __builtin_amdgcn_exp2f(m - ms), f1 = __builtin_amdgcn_exp2f(m1 - ms);
-    l = fmaf(l, f0, ml[64 + lane] * f1);
-    m = mn;
+    if (group > 0) return;
+#pragma unroll 1
+    for (int g = 1; g < GROUPS; ++g) {
+      const float *from = part(g) + lane * 4, *ml = part(g) + DT * 1024 + lane;
+      const float m1 = ml[0], mn = fmaxf(m, m1), ms = mn == -INFINITY ? 0.f : mn;
+      const float f0 = __builtin_amdgcn_exp2f(m - ms), f1 = __builtin_amdgcn_exp2f(m1 - ms);
+      l = fmaf(l, f0, ml[64] * f1);
+      m = mn;
 #pragma unroll
-    for (int d = 0; d < DT; ++d)
+      for (int d = 0; d < DT; ++d)
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const f32x4 x = *reinterpret_cast<const f32x4*>(part + (d * 4 + q) * 256);
+        for (int q = 0; q < 4; ++q) {
+          const f32x4 x = *reinterpret_cast<const f32x4*>(from + (d * 4 + q) * 256);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) o[d][4 * q + e] = fmaf(o[d][4 * q + e], f0, x[e] * f1);
-      }
+          for (int e = 0; e < 4; ++e) o[d][4 * q + e] = fmaf(o[d][4 * q + e], f0, x[e] * f1);
+        }
+    }
     wave_lds_fence();
   }
   if (i0 >= nq) return;
   const float inv = l == 0.f ? 0.f : 1.f / l;
   if (lse && h == 0 && i0 + i < nq) lse[mine] = (m + __builtin_amdgcn_logf(l)) * kLn2;
-  // rows out as whole lines, through the ring buffer that the last tile is not in (two groups: where the wavefront's sums were)
-  const uint32_t out = GROUPS == 2 ? wave * (DT * 4096 + 512) : (ntile & 1) * 2 * TILE_BYTES + wave * (32 * DH * 2);
+  // rows out as whole lines, through the ring buffer that the last tile is not in (several groups: where the first other's sums were)
+  const uint32_t out = GROUPS > 1 ? wave * Sizes::PART : (ntile & 1) * 2 * TILE_BYTES + wave * (32 * DH * 2);
 #pragma unroll
   for (int d = 0; d < DT; ++d) {
     float v[16];
@@ -251,12 +266,16 @@ bool two_groups(const spt_attn_shape_t& s, int hshift) {
   return workgroups <= resident / 2 || (workgroups <= resident && s.Tk >= 1024 * (int64_t)s.B);
 }
 
-template <int DH, int GROUPS>
-hipError_t launch_fwd(const FwdArgs& a, int grid, hipStream_t st) {
-  constexpr int smem = GROUPS * 4 * kTileKeys * DH * 2;
+template <int DH, int OWNERS, int GROUPS>
+hipError_t launch_fwd(FwdArgs a, const spt_attn_shape_t& s, hipStream_t st) {
+  typedef FwdSizes<DH, OWNERS, GROUPS> Sizes;
+  const auto kernel = prompt_fwd_kernel<DH, OWNERS, GROUPS>;
   static std::atomic<uint64_t> done{0};
-  if (const hipError_t e = allow_smem(reinterpret_cast<const void*>(prompt_fwd_kernel<DH, GROUPS>), smem, done); e != hipSuccess) return e;
-  hipLaunchKernelGGL((prompt_fwd_kernel<DH, GROUPS>), dim3(grid), dim3(256 * GROUPS), smem, st, a);
+  if (const hipError_t e = allow_smem(reinterpret_cast<const void*>(kernel), Sizes::SMEM, done); e != hipSuccess) return e;
+  if (OWNERS == 1) a.hshift = 0;
+  const int heads = a.G >> a.hshift, tiles = s.Tq >> (Sizes::SHIFT - a.hshift);
+  a.coarse = coarse_tiles((int64_t)tiles * heads * s.Hk, DH == 128 ? 2 : 4);
+  hipLaunchKernelGGL(kernel, dim3(head_item_grid(s.Hk, (tiles + s.B) * heads)), dim3(64 * OWNERS * GROUPS), Sizes::SMEM, st, a);   // (so many tiles at most)
   return hipGetLastError();
 }
 
@@ -296,14 +315,16 @@ extern "C" int spt_attn_prompt_fwd(const spt_attn_shape_t* shape, const void* Q,
   a.cu_q = cu_q; a.cu_k = cu_k; a.lse = lse;
   a.B = s.B; a.Tq = s.Tq; a.Tk = s.Tk; a.Hk = s.Hk; a.G = s.H / s.Hk;
   a.hshift = attn_heads_shift(a.G);
-  const int grid = head_item_grid(s.Hk, ((s.Tq >> (7 - a.hshift)) + s.B) * (a.G >> a.hshift));   // (tiles: so many at most)
   a.causal = s.causal;
-  a.coarse = coarse_tiles((int64_t)(s.Tq >> (7 - a.hshift)) * (s.H >> a.hshift), s.dh == 128 ? 2 : 4);
   a.c = s.scale * kLog2e;
   const hipStream_t st = static_cast<hipStream_t>(stream);
   ScopedKernelTimer timer(kSlotAttnFwd, st);
-  const bool two = two_groups(s, a.hshift);
-  const hipError_t e = s.dh == 128 ? (two ? launch_fwd<128, 2>(a, grid, st) : launch_fwd<128, 1>(a, grid, st))
-                                   : (two ? launch_fwd<64, 2>(a, grid, st) : launch_fwd<64, 1>(a, grid, st));
+  const auto launch = [&](auto dh) {
+    constexpr int DH = decltype(dh)::value;
+    const int64_t tiles = (int64_t)(s.Tq >> (7 - a.hshift)) * (s.H >> a.hshift);
+    if (split_rows(tiles, s.Tk, s.B)) return launch_fwd<DH, 1, DH == 128 ? 4 : 8>(a, s, st);
+    return two_groups(s, a.hshift) ? launch_fwd<DH, 4, 2>(a, s, st) : launch_fwd<DH, 4, 1>(a, s, st);
+  };
+  const hipError_t e = s.dh == 128 ? launch(std::integral_constant<int, 128>()) : launch(std::integral_constant<int, 64>());
   return e == hipSuccess ? SPT_OK : SPT_ERR_HIP;
 }

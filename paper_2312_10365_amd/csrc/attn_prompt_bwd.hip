@@ -10,14 +10,17 @@
 //   prompt_bwd_kv_kernel  a wavefront owns 32 keys of a key head, the queries of all heads of its group pass through LDS in tiles
 //                         of 32, heads outermost, so a gradient is summed in one fixed order: S and dP with the key side in
 //                         registers, dV^T += dY^T P, dK^T += Q^T dS.
+// Where there is little to do, four or eight wavefronts share what passes through LDS for the same 32 rows, and their sums are added in order.
 // S and dP are formed in both: the alternative, keeping dS or partial dQ in memory, moves as many bytes as it saves time.
+#include <type_traits>
+
 #include "attn_common.hpp"
 
 using namespace spt;
 
 namespace {
 
-constexpr int kTile = 32, kOwnKeys = 128;   // rows of a tile that passes through LDS; keys of a workgroup
+constexpr int kTile = 32;                   // rows of a tile that passes through LDS; rows of a wavefront
 constexpr int kRing = 2;                    // tiles in LDS: one in use, one being filled
 
 struct BwdArgs {
@@ -45,8 +48,6 @@ struct Weights<true> { u32x4 p[2], ds[2], rest[2]; };
 // up to 80, 1.45 for longer ones, 1.0 exact.  Key side, us, rounded and exact: 8192 tokens, 32 heads of 128 on 8: sequences of 32 95 and 99,
 // of 64 71 and 75, of 128 61 and 65; 32 heads of 64: 57 and 58, 44 and 47, 46 and 48, of 512 67 and 76.
 constexpr int kFewRows = 128;     // of queries of a sequence and key head, on average
-constexpr int kFewInAll = 8192;   // of queries and heads
-
 
 // p and dS of one pair, from its rows in memory.
 struct PairGrad { float p, ds; };
@@ -55,17 +56,17 @@ __device__ __forceinline__ PairGrad pair_grad(const char* q, const char* k, cons
   return {p, p * (row_dot(dy, v, dh) - D)};
 }
 
-// Rows q0 .. q0 + 31 of two tensors of n rows into a pair of tiles (rows past the end: the last one again).
-template <int DH>
+// Rows q0 .. q0 + 31 of two tensors of n rows into a pair of tiles (rows past the end: the last one again), by WAVES wavefronts.
+template <int DH, int WAVES>
 __device__ __forceinline__ void fetch_pair(int tid, const char* x, int64_t xrow, const char* y, int64_t yrow, int q0, int n, const char* tiles, int wave) {
-  constexpr int COPIES = kTile * (DH / 8) / 256;
+  constexpr int COPIES = kTile * (DH / 8) / (64 * WAVES);
   const char* xb = x + q0 * xrow;
   const char* yb = y + q0 * yrow;
 #pragma unroll
   for (int u = 0; u < COPIES; ++u) {
-    const int slot = u * 256 + tid, r0 = slot / (DH / 8);
+    const int slot = u * 64 * WAVES + tid, r0 = slot / (DH / 8);
     const uint32_t chunk = ((slot % (DH / 8)) ^ row_swizzle<DH>(r0)) * 16, r = (uint32_t)min(r0, n - 1 - q0);
-    const uint32_t at = lds_addr(tiles + u * 4096 + wave * 1024);
+    const uint32_t at = lds_addr(tiles + (u * WAVES + wave) * 1024);
     dma16_at(xb, r * (uint32_t)xrow + chunk, at);
     dma16_at(yb, r * (uint32_t)yrow + chunk, at + kTile * DH * 2);
   }
@@ -89,14 +90,63 @@ __device__ __forceinline__ void slow_dq_row(const BwdArgs& a, const char* q, con
   for (int d = 0; d < DH / 64; ++d) reinterpret_cast<uint16_t*>(dq)[lane + 64 * d] = (uint16_t)pack_bf16x2(acc[d] * a.scale, 0.f);
 }
 
-template <int DH, bool EXACT>
-__global__ __launch_bounds__(256, 2) void prompt_bwd_q_kernel(const BwdArgs a) {
-  constexpr int KS = DH / 16, DT = DH / 32, TILE_BYTES = kTile * DH * 2;
-  // 128-wide heads: dY of the wavefront's rows stays in LDS, or two wavefronts would not fit into a SIMD's registers
-  constexpr bool OWN = DH == 128;
-  __shared__ __align__(256) char smem[(kRing * 2 + (OWN ? 4 : 0)) * TILE_BYTES];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 31, h = lane >> 5;
-  const int hsets = a.G >> a.hshift, pshift = 7 - a.hshift;
+// Sizes of a workgroup of GROUPS groups of OWNERS wavefronts.  A wavefront of a group owns 32 rows, the groups go through every GROUPS-th
+// tile for the same rows.
+template <int DH, int OWNERS, int GROUPS>
+struct BwdSizes {
+  static constexpr int TILE_BYTES = kTile * DH * 2, SHIFT = OWNERS == 4 ? 7 : 5, THREADS = 64 * OWNERS * GROUPS;   // 1 << SHIFT: rows
+  // 128-wide heads: a row operand of the wavefront's own stays in LDS, or two wavefronts would not fit into a SIMD's registers
+  static constexpr bool OWN = DH == 128;
+  static constexpr int OWN_BYTES = OWN ? OWNERS * TILE_BYTES : 0;
+  static constexpr int SUMS = (GROUPS - 1) * OWNERS * DH * 128;                 // a gradient of the other groups
+  static constexpr int Q_RING = kRing * 2 * TILE_BYTES;                         // of a group: tiles of K and V
+  static constexpr int Q_JOIN = SUMS + (GROUPS - 1) * OWNERS * 512, Q_RINGS = GROUPS * Q_RING + OWN_BYTES;
+  static constexpr int Q_SMEM = Q_RINGS > Q_JOIN ? Q_RINGS : Q_JOIN;
+  static constexpr int KV_RING = kRing * (2 * TILE_BYTES + 256);                // tiles of Q and dY, their rows' offsets and -D
+  static constexpr int KV_SMEM = GROUPS * KV_RING + OWN_BYTES;
+  static_assert(Q_SMEM <= 160 * 1024 && KV_SMEM <= 160 * 1024 && SUMS <= GROUPS * KV_RING, "a CU's LDS");
+};
+
+// The other groups' sums of `sum` (and of two numbers a lane) are added to the first's, in order.  All wavefronts of the workgroup.
+template <int DH, int OWNERS, int GROUPS>
+__device__ __forceinline__ void add_groups(f32x16* sum, char* smem, int wave, int group, int lane) {
+  constexpr int DT = DH / 32;
+  float* mine = reinterpret_cast<float*>(smem) + ((group - 1) * OWNERS + wave) * (DT * 1024) + lane * 4;
+  __syncthreads();
+  if (group > 0) {
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        *reinterpret_cast<f32x4*>(mine + (d * 4 + q) * 256) = f32x4{sum[d][4 * q], sum[d][4 * q + 1], sum[d][4 * q + 2], sum[d][4 * q + 3]};
+  }
+  __syncthreads();
+  if (group == 0) {
+#pragma unroll 1
+    for (int g = 1; g < GROUPS; ++g) {
+      const float* half = reinterpret_cast<float*>(smem) + ((g - 1) * OWNERS + wave) * (DT * 1024) + lane * 4;
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const f32x4 x = *reinterpret_cast<const f32x4*>(half + (d * 4 + q) * 256);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sum[d][4 * q + e] += x[e];
+        }
+    }
+  }
+}
+
+template <int DH, int OWNERS, int GROUPS, bool EXACT>
+__global__ __launch_bounds__((64 * OWNERS * GROUPS), (OWNERS == 1 && DH == 128 ? 1 : 2)) void prompt_bwd_q_kernel(const BwdArgs a) {
+  typedef BwdSizes<DH, OWNERS, GROUPS> Sizes;
+  constexpr int KS = DH / 16, DT = DH / 32, TILE_BYTES = Sizes::TILE_BYTES;
+  constexpr bool OWN = Sizes::OWN;
+  extern __shared__ __align__(256) char smem[];
+  const int lane = threadIdx.x & 63, i = lane & 31, h = lane >> 5, tid = threadIdx.x % (64 * OWNERS);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % OWNERS, group = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) / OWNERS;
+  char* ring = smem + group * Sizes::Q_RING;
+  const int hsets = a.G >> a.hshift, pshift = Sizes::SHIFT - a.hshift;
   const HeadItem w = head_item(blockIdx.x, a.Hk);
   const int hk = w.hk, hs = w.item % hsets;
   TilePlace at;
@@ -117,8 +167,8 @@ __global__ __launch_bounds__(256, 2) void prompt_bwd_q_kernel(const BwdArgs a) {
 
   const char* kbase = a.K.p + (int64_t)sk.first * a.K.row + (int64_t)hk * a.K.head;
   const char* vbase = a.V.p + (int64_t)sk.first * a.V.row + (int64_t)hk * a.V.head;
-  auto fetch = [&](int t) { fetch_pair<DH>(threadIdx.x, kbase, a.K.row, vbase, a.V.row, t * kTile, nk, smem + t % kRing * 2 * TILE_BYTES, wave); };
-  if (ntile > 0) fetch(0);
+  auto fetch = [&](int t, int buf) { fetch_pair<DH, OWNERS>(tid, kbase, a.K.row, vbase, a.V.row, t * kTile, nk, ring + buf * 2 * TILE_BYTES, wave); };
+  if (group < ntile) fetch(group, 0);
 
   const int64_t row = sq.first + mine;
   const char* qrow = a.Q.p + row * a.Q.row + (int64_t)head * a.Q.head;
@@ -126,14 +176,17 @@ __global__ __launch_bounds__(256, 2) void prompt_bwd_q_kernel(const BwdArgs a) {
   const char* dyrow = a.dY.p + row * a.dY.row + (int64_t)head * a.dY.head;
   bf16x8 qf[KS], dyf[OWN ? 1 : KS];
   TileReader<DH> lds(lane);
-  const uint32_t tiles = lds_addr(smem), own = tiles + (kRing * 2 + wave) * TILE_BYTES;
+  const uint32_t tiles = lds_addr(ring), own = lds_addr(smem) + GROUPS * Sizes::Q_RING + wave * TILE_BYTES;
   float D = 0.f;
 #pragma unroll
   for (int s = 0; s < KS; ++s) {
     qf[s] = *reinterpret_cast<const bf16x8*>(qrow + s * 32 + h * 16);
     const u32x4 dy = *reinterpret_cast<const u32x4*>(dyrow + s * 32 + h * 16), y = *reinterpret_cast<const u32x4*>(yrow + s * 32 + h * 16);
-    if (OWN) *reinterpret_cast<u32x4*>(smem + (kRing * 2 + wave) * TILE_BYTES + (lds.row ^ (uint32_t)(s * 32))) = dy;
-    else dyf[s] = as_bf16x8(dy);
+    if (OWN) {   // (every group the same)
+      *reinterpret_cast<u32x4*>(smem + GROUPS * Sizes::Q_RING + wave * TILE_BYTES + (lds.row ^ (uint32_t)(s * 32))) = dy;
+    } else {
+      dyf[s] = as_bf16x8(dy);
+    }
 #pragma unroll
     for (int e = 0; e < 4; ++e) D = fmaf(hi_bf16(dy[e]), hi_bf16(y[e]), fmaf(lo_bf16(dy[e]), lo_bf16(y[e]), D));
   }
@@ -148,8 +201,7 @@ __global__ __launch_bounds__(256, 2) void prompt_bwd_q_kernel(const BwdArgs a) {
   float left_over = 0.f, rounded = 0.f;                  // sum of dS: what D lacks; of dS as rounded
   NotFinite not_finite;
 
-  auto first_products = [&](int t, f32x16& s, f32x16& dp) {
-    const uint32_t kt = tiles + (t % kRing) * 2 * TILE_BYTES;
+  auto first_products = [&](uint32_t kt, f32x16& s, f32x16& dp) {
     lds.fresh();
 #pragma unroll
     for (int r = 0; r < 16; ++r) s[r] = dp[r] = 0.f;
@@ -187,8 +239,7 @@ __global__ __launch_bounds__(256, 2) void prompt_bwd_q_kernel(const BwdArgs a) {
     }
     return w;
   };
-  auto second_products = [&](int t, const Weights<EXACT>& w) {
-    const uint32_t kt = tiles + (t % kRing) * 2 * TILE_BYTES;
+  auto second_products = [&](uint32_t kt, const Weights<EXACT>& w) {
     lds.fresh();
 #pragma unroll
     for (int half = 0; half < 2; ++half)
@@ -200,31 +251,30 @@ __global__ __launch_bounds__(256, 2) void prompt_bwd_q_kernel(const BwdArgs a) {
         mean[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, as_bf16x8(w.p[half]), mean[d], 0, 0, 0);
       }
   };
-  auto turn = [&](int t) {                               // tile t is there; asks for the next
-    wait_vmcnt<0>();
+  for (int t0 = 0; t0 < ntile; t0 += GROUPS) {
+    wait_vmcnt<0>();                                     // the group's tile is there; asks for its next one
     __syncthreads();
-    if (t + 1 < ntile) fetch(t + 1);
-  };
-  for (int t = 0; t < ntile; ++t) {
-    turn(t);
-    const int j0 = t * kTile;
+    const int t = t0 + group, buf = t0 / GROUPS % kRing, j0 = t * kTile;
+    const uint32_t kt = tiles + buf * 2 * TILE_BYTES;
+    if (t + GROUPS < ntile) fetch(t + GROUPS, buf ^ 1);
+    if (t >= ntile) continue;
     if (j0 + kTile > full) {
 #pragma unroll
-      for (int u = 0; u < TILE_BYTES / 4096; ++u) not_finite.look(lds_read<u32x4>(tiles + t % kRing * 2 * TILE_BYTES + u * 4096 + threadIdx.x * 16));
+      for (int u = 0; u < TILE_BYTES / (1024 * OWNERS); ++u) not_finite.look(lds_read<u32x4>(kt + u * 1024 * OWNERS + tid * 16));
     }
     if (j0 >= wave_kend) continue;
     const bool masked = j0 + kTile > wave_full;
     __builtin_amdgcn_iglp_opt(1);                        // (reads of LDS between the products: see the forward)
     f32x16 s, dp;
-    first_products(t, s, dp);
-    second_products(t, weights(t, s, dp, masked));
+    first_products(kt, s, dp);
+    second_products(kt, weights(t, s, dp, masked));
   }
   left_over += other_half(left_over);
   rounded = EXACT ? left_over : rounded + other_half(rounded);
   const int64_t stat = (int64_t)head * a.Tq;
   // rows that not all queries may see hold infinities or NaN: 0 times those is NaN
   if (full < ntile * kTile && __syncthreads_or(not_finite.found())) {
-    for (int r = 0; r < min(32, nq - i0); ++r) {
+    for (int r = group; r < min(32, nq - i0); r += GROUPS) {
       const int64_t at = sq.first + i0 + r;
       const float Dr = __shfl(D, r), offr = __shfl(off, r);
       if (lane == 0) {
@@ -235,6 +285,21 @@ __global__ __launch_bounds__(256, 2) void prompt_bwd_q_kernel(const BwdArgs a) {
                       a.causal ? min(nk, i0 + r + ahead + 1) : nk, offr, Dr, a.dQ.p + at * a.dQ.row + (int64_t)head * a.dQ.head);
     }
     return;
+  }
+  if (GROUPS > 1) {
+    add_groups<DH, OWNERS, GROUPS>(o, smem, wave, group, lane);
+    add_groups<DH, OWNERS, GROUPS>(mean, smem, wave, group, lane);
+    float* rest = reinterpret_cast<float*>(smem + Sizes::SUMS) + wave * 128 + lane;
+    if (group > 0) {
+      rest[(group - 1) * OWNERS * 128] = left_over;
+      rest[(group - 1) * OWNERS * 128 + 64] = rounded;
+    }
+    __syncthreads();
+    if (group > 0) return;
+    for (int g = 0; g < GROUPS - 1; ++g) {
+      left_over += rest[g * OWNERS * 128];
+      rounded += rest[g * OWNERS * 128 + 64];
+    }
   }
   if (i0 + i >= nq) return;
   if (h == 0) {
@@ -283,39 +348,29 @@ __device__ __forceinline__ void slow_dkv_row(const BwdArgs& a, const SeqRows& sq
   }
 }
 
-// Sizes of the key side: GROUPS groups of four wavefronts go through every GROUPS-th step, on the same 128 keys.
-template <int DH, int GROUPS>
-struct KvSizes {
-  static constexpr int TILE_BYTES = kTile * DH * 2, STAT = 256;
-  static constexpr bool OWN = DH == 128;                         // V of the keys stays in LDS: registers, as above
-  static constexpr int RING = kRing * (2 * TILE_BYTES + STAT);   // of a group: tiles of Q and dY, their rows' offsets and -D
-  static constexpr int SMEM = GROUPS * RING + (OWN ? 4 * TILE_BYTES : 0);
-  static_assert(GROUPS == 1 || GROUPS * RING >= 4 * DH * 32 * 4, "a gradient of the second group passes through LDS");
-};
-
-template <int DH, int GROUPS, bool EXACT>
-__global__ __launch_bounds__(256 * GROUPS, 2) void prompt_bwd_kv_kernel(const BwdArgs a) {
-  typedef KvSizes<DH, GROUPS> Sizes;
-  constexpr int KS = DH / 16, DT = DH / 32, TILE_BYTES = Sizes::TILE_BYTES;
+template <int DH, int OWNERS, int GROUPS, bool EXACT>
+__global__ __launch_bounds__((64 * OWNERS * GROUPS), (OWNERS == 1 && DH == 128 ? 1 : 2)) void prompt_bwd_kv_kernel(const BwdArgs a) {
+  typedef BwdSizes<DH, OWNERS, GROUPS> Sizes;
+  constexpr int KS = DH / 16, DT = DH / 32, TILE_BYTES = Sizes::TILE_BYTES, OWN_KEYS = kTile * OWNERS;
   constexpr bool OWN = Sizes::OWN;
   extern __shared__ __align__(256) char smem[];
-  const int lane = threadIdx.x & 63, i = lane & 31, h = lane >> 5, tid = threadIdx.x & 255;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) & 3, group = GROUPS == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 8);
-  char* ring = smem + group * Sizes::RING;
+  const int lane = threadIdx.x & 63, i = lane & 31, h = lane >> 5, tid = threadIdx.x % (64 * OWNERS);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % OWNERS, group = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) / OWNERS;
+  char* ring = smem + group * Sizes::KV_RING;
   float* stats = reinterpret_cast<float*>(ring + kRing * 2 * TILE_BYTES);
   const HeadItem w = head_item(blockIdx.x, a.Hk);
   const int hk = w.hk;
   TilePlace place;
-  if (!find_tile<true>(a.cu_k, a.cu_q, a.B, a.Tk, a.Tq, 7, a.causal, a.coarse, w.item, place)) return;
+  if (!find_tile<true>(a.cu_k, a.cu_q, a.B, a.Tk, a.Tq, Sizes::SHIFT, a.causal, a.coarse, w.item, place)) return;
   const int tile = place.tile;
   const SeqRows sk = place.own, sq = place.other;
   const int nq = sq.n, nk = sk.n, ahead = nk - nq;
-  const int j0 = tile * kOwnKeys + wave * 32, mine = min(j0 + i, nk - 1);
+  const int j0 = tile * OWN_KEYS + wave * 32, mine = min(j0 + i, nk - 1);
   const int first = a.causal ? max(0, mine - ahead) : 0;                 // the first query that sees the lane's key
-  const int begin = a.causal ? max(0, tile * kOwnKeys - ahead) & ~(kTile - 1) : 0;
+  const int begin = a.causal ? max(0, tile * OWN_KEYS - ahead) & ~(kTile - 1) : 0;
   // Tiles of a head from `begin` on: in front of `full` some query does not see some key of the workgroup, the last one may be
   // short, the others need no mask.  Steps: the masked tiles of all heads, then the others.
-  const int full = a.causal ? max(begin, (tile * kOwnKeys + kOwnKeys - 1 - ahead + kTile - 1) & ~(kTile - 1)) : 0;
+  const int full = a.causal ? max(begin, (tile * OWN_KEYS + OWN_KEYS - 1 - ahead + kTile - 1) & ~(kTile - 1)) : 0;
   const int tail = nq & ~(kTile - 1), front = max(0, min(full, nq) - begin + kTile - 1) / kTile;
   const int head_masked = front + (tail < nq && tail >= full), head_full = max(0, tail - full) / kTile;
   const int masked_steps = head_masked * a.G, steps = masked_steps + head_full * a.G;
@@ -329,21 +384,21 @@ __global__ __launch_bounds__(256 * GROUPS, 2) void prompt_bwd_kv_kernel(const Bw
   };
   auto fetch = [&](int t, const Place& p) {
     const int head = hk * a.G + p.g, q0 = first_query(t, p), buf = t / GROUPS % kRing;
-    fetch_pair<DH>(tid, a.Q.p + (int64_t)sq.first * a.Q.row + (int64_t)head * a.Q.head, a.Q.row,
+    fetch_pair<DH, OWNERS>(tid, a.Q.p + (int64_t)sq.first * a.Q.row + (int64_t)head * a.Q.head, a.Q.row,
                    a.dY.p + (int64_t)sq.first * a.dY.row + (int64_t)head * a.dY.head, a.dY.row, q0, nq, ring + buf * 2 * TILE_BYTES, wave);
     const int64_t at = (int64_t)head * a.Tq + sq.first + q0 + min(i, nq - 1 - q0);
     if (wave == 0) dma4(h ? a.neg_d + at : a.off + at, lds_addr(stats + buf * 64));
   };
   // the group's steps: group, group + GROUPS, ...
   Place here = {0, 0}, coming;
-  if (group == 1) here = after(0, here);
+  for (int n = 0; n < group; ++n) here = after(n, here);
   coming = here;
   if (group < steps) fetch(group, here);
 
   bf16x8 kf[KS], vf[OWN ? 1 : KS];
   TileReader<DH> lds(lane);
-  const uint32_t tiles = lds_addr(ring), own = lds_addr(smem) + GROUPS * Sizes::RING + wave * TILE_BYTES;
-  char* own_tile = smem + GROUPS * Sizes::RING + wave * TILE_BYTES;
+  const uint32_t tiles = lds_addr(ring), own = lds_addr(smem) + GROUPS * Sizes::KV_RING + wave * TILE_BYTES;
+  char* own_tile = smem + GROUPS * Sizes::KV_RING + wave * TILE_BYTES;
   if (!OWN) {
     const char* krow = a.K.p + (int64_t)(sk.first + mine) * a.K.row + (int64_t)hk * a.K.head;
     const char* vrow = a.V.p + (int64_t)(sk.first + mine) * a.V.row + (int64_t)hk * a.V.head;
@@ -451,7 +506,7 @@ __global__ __launch_bounds__(256 * GROUPS, 2) void prompt_bwd_kv_kernel(const Bw
     const bool masked = t < masked_steps;
     if (masked) {
 #pragma unroll
-      for (int u = 0; u < 2 * TILE_BYTES / 4096; ++u) not_finite.look(lds_read<u32x4>(tiles + buf * 2 * TILE_BYTES + u * 4096 + tid * 16));
+      for (int u = 0; u < 2 * TILE_BYTES / (1024 * OWNERS); ++u) not_finite.look(lds_read<u32x4>(tiles + buf * 2 * TILE_BYTES + u * 1024 * OWNERS + tid * 16));
     }
     if (q0 < wave_begin) continue;
     const bool cut = masked && ((a.causal && q0 < j0 + 31 - ahead) || q0 + kTile > nq);   // (some query of the tile does not see some key of the wavefront)
@@ -470,32 +525,10 @@ __global__ __launch_bounds__(256 * GROUPS, 2) void prompt_bwd_kv_kernel(const Bw
     }
     return;
   }
-  if (GROUPS == 2) {                                                     // the second group's sums, one gradient at a time
-    float* half = reinterpret_cast<float*>(smem) + wave * (DT * 1024) + lane * 4;
-#pragma unroll
-    for (int n = 0; n < 2; ++n) {
-      f32x16* sum = n == 0 ? ok : ov;
-      __syncthreads();
-      if (group == 1) {
-#pragma unroll
-        for (int d = 0; d < DT; ++d)
-#pragma unroll
-          for (int q = 0; q < 4; ++q)
-            *reinterpret_cast<f32x4*>(half + (d * 4 + q) * 256) = f32x4{sum[d][4 * q], sum[d][4 * q + 1], sum[d][4 * q + 2], sum[d][4 * q + 3]};
-      }
-      __syncthreads();
-      if (group == 0) {
-#pragma unroll
-        for (int d = 0; d < DT; ++d)
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            const f32x4 x = *reinterpret_cast<const f32x4*>(half + (d * 4 + q) * 256);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) sum[d][4 * q + e] += x[e];
-          }
-      }
-    }
-    if (group == 1) return;
+  if (GROUPS > 1) {
+    add_groups<DH, OWNERS, GROUPS>(ok, smem, wave, group, lane);
+    add_groups<DH, OWNERS, GROUPS>(ov, smem, wave, group, lane);
+    if (group > 0) return;
   }
   if (!OWN) {
     if (j0 + i >= nk) return;
@@ -532,12 +565,30 @@ __global__ __launch_bounds__(256 * GROUPS, 2) void prompt_bwd_kv_kernel(const Bw
   }
 }
 
-template <int DH, int GROUPS, bool EXACT>
-hipError_t launch_kv(const BwdArgs& a, int grid, hipStream_t st) {
-  constexpr int smem = KvSizes<DH, GROUPS>::SMEM;
+template <int DH, int OWNERS, int GROUPS, bool EXACT>
+hipError_t launch_q(BwdArgs a, const spt_attn_shape_t& s, hipStream_t st) {
+  typedef BwdSizes<DH, OWNERS, GROUPS> Sizes;
+  const auto kernel = prompt_bwd_q_kernel<DH, OWNERS, GROUPS, EXACT>;
   static std::atomic<uint64_t> done{0};
-  if (const hipError_t e = allow_smem(reinterpret_cast<const void*>(prompt_bwd_kv_kernel<DH, GROUPS, EXACT>), smem, done); e != hipSuccess) return e;
-  hipLaunchKernelGGL((prompt_bwd_kv_kernel<DH, GROUPS, EXACT>), dim3(grid), dim3(256 * GROUPS), smem, st, a);
+  if (const hipError_t e = allow_smem(reinterpret_cast<const void*>(kernel), Sizes::Q_SMEM, done); e != hipSuccess) return e;
+  if (OWNERS == 1) a.hshift = 0;
+  const int heads = a.G >> a.hshift, tiles = s.Tq >> (Sizes::SHIFT - a.hshift);
+  a.coarse = coarse_tiles((int64_t)tiles * heads * s.Hk, DH == 128 ? 2 : 3);
+  hipLaunchKernelGGL(kernel, dim3(head_item_grid(s.Hk, (tiles + s.B) * heads)), dim3(64 * OWNERS * GROUPS), Sizes::Q_SMEM, st, a);
+  return hipGetLastError();
+}
+
+template <int DH, int OWNERS, int GROUPS, bool EXACT>
+hipError_t launch_kv(BwdArgs a, const spt_attn_shape_t& s, hipStream_t st) {
+  typedef BwdSizes<DH, OWNERS, GROUPS> Sizes;
+  const auto kernel = prompt_bwd_kv_kernel<DH, OWNERS, GROUPS, EXACT>;
+  static std::atomic<uint64_t> done{0};
+  if (const hipError_t e = allow_smem(reinterpret_cast<const void*>(kernel), Sizes::KV_SMEM, done); e != hipSuccess) return e;
+  const int tiles = s.Tk >> Sizes::SHIFT;
+  // (heads that share their keys make fewer and longer tiles, of which the order by work alone is better: us, 48 sequences of 512, 32 heads of
+  // 128 on 8 318 and 410 so, on 16 385 and 381, on 32 496 and 445)
+  a.coarse = a.G > 1 ? 0 : coarse_tiles((int64_t)tiles * s.Hk, DH == 128 ? 1 : 3);
+  hipLaunchKernelGGL(kernel, dim3(head_item_grid(s.Hk, tiles + s.B)), dim3(64 * OWNERS * GROUPS), Sizes::KV_SMEM, st, a);
   return hipGetLastError();
 }
 
@@ -572,23 +623,22 @@ extern "C" int spt_attn_prompt_bwd(const spt_attn_shape_t* shape, const void* Q,
   a.causal = s.causal;
   a.scale = s.scale;
   a.c = s.scale * kLog2e;
-  const bool few = (int64_t)s.Tq * a.G <= (int64_t)kFewRows * s.B || (int64_t)s.Tq * s.H <= kFewInAll;
+  const int64_t q_tiles = (int64_t)(s.Tq >> (7 - a.hshift)) * (s.H >> a.hshift), kv_tiles = (int64_t)(s.Tk >> 7) * s.Hk;
+  const bool few = (int64_t)s.Tq * a.G <= (int64_t)kFewRows * s.B || q_tiles <= kFewTiles;
+  const bool split_q = split_rows(q_tiles, s.Tk, s.B), split_kv = split_rows(kv_tiles, (int64_t)s.Tq * a.G, s.B);
   const hipStream_t st = static_cast<hipStream_t>(stream);
-  {
-    ScopedKernelTimer timer(kSlotAttnBwdQ, st);
-    a.coarse = coarse_tiles((int64_t)(s.Tq >> (7 - a.hshift)) * (s.H >> a.hshift), s.dh == 128 ? 2 : 3);
-    const int grid = head_item_grid(s.Hk, ((s.Tq >> (7 - a.hshift)) + s.B) * (a.G >> a.hshift));
-    const auto kernel = s.dh == 128 ? (few ? prompt_bwd_q_kernel<128, true> : prompt_bwd_q_kernel<128, false>)
-                                    : (few ? prompt_bwd_q_kernel<64, true> : prompt_bwd_q_kernel<64, false>);
-    hipLaunchKernelGGL(kernel, dim3(grid), dim3(256), 0, st, a);
-    if (hipGetLastError() != hipSuccess) return SPT_ERR_HIP;
-  }
-  ScopedKernelTimer timer(kSlotAttnBwdKV, st);
-  // (heads that share their keys make fewer and longer tiles, of which the order by work alone is better: us, 48 sequences of 512, 32 heads of
-  // 128 on 8 318 and 410 so, on 16 385 and 381, on 32 496 and 445)
-  a.coarse = a.G > 1 ? 0 : coarse_tiles((int64_t)(s.Tk / kOwnKeys) * s.Hk, s.dh == 128 ? 1 : 3);
-  const int grid = head_item_grid(s.Hk, s.Tk / kOwnKeys + s.B);
-  const hipError_t e = s.dh == 128 ? (few ? launch_kv<128, 2, true>(a, grid, st) : launch_kv<128, 2, false>(a, grid, st))
-                                   : (few ? launch_kv<64, 1, true>(a, grid, st) : launch_kv<64, 1, false>(a, grid, st));
+  const auto launches = [&](auto dh, auto exact) {
+    constexpr int DH = decltype(dh)::value, SPLIT = DH == 128 ? 4 : 8;
+    constexpr bool EXACT = decltype(exact)::value;
+    {
+      ScopedKernelTimer timer(kSlotAttnBwdQ, st);
+      if (const hipError_t e = split_q ? launch_q<DH, 1, SPLIT, true>(a, s, st)   // (so few are exact)
+                                        : launch_q<DH, 4, 1, EXACT>(a, s, st); e != hipSuccess) return e;
+    }
+    ScopedKernelTimer timer(kSlotAttnBwdKV, st);
+    return split_kv ? launch_kv<DH, 1, SPLIT, EXACT>(a, s, st) : launch_kv<DH, 4, DH == 128 ? 2 : 1, EXACT>(a, s, st);
+  };
+  const auto of = [&](auto dh) { return few ? launches(dh, std::true_type()) : launches(dh, std::false_type()); };
+  const hipError_t e = s.dh == 128 ? of(std::integral_constant<int, 128>()) : of(std::integral_constant<int, 64>());
   return e == hipSuccess ? SPT_OK : SPT_ERR_HIP;
 }

@@ -83,6 +83,25 @@ def test_prompt(name):
     check_prompt(out, want_prompt(lens_q, lens_k, causal, Q, K, V, dY), sum(lens_q), sum(lens_k))
 
 
+FEW = {   # few workgroups with much to read: rows in 32s, or on one side only
+    "two_heads": ([300, 0, 451], [300, 0, 451], 2, 2, True),
+    "two_heads_full": ([1, 640], [70, 640], 2, 2, False),
+    "one_key_head": ([500, 233], [500, 233], 12, 1, True),
+    "one_key_head_full": ([129, 400], [400, 129], 6, 1, False),
+    "part_of_a_prompt": ([40, 1], [1000, 700], 4, 2, True),
+    "more_queries": ([700, 31], [50, 300], 3, 3, True),
+}
+
+
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("name", FEW)
+def test_prompt_few(name, dh):
+    lens_q, lens_k, H, Hk, causal = FEW[name]
+    Q, K, V, dY = prompt_inputs(lens_q, lens_k, H, Hk, dh, seed=71)
+    out = run_prompt(lens_q, lens_k, causal, *(t.cuda() for t in (Q, K, V, dY)))
+    check_prompt(out, want_prompt(lens_q, lens_k, causal, Q, K, V, dY), sum(lens_q), sum(lens_k))
+
+
 LARGE = {   # more workgroups than are resident at once; gradients summed over many rows
     "many_heads_64": ([333, 65, 0, 200, 500], [333, 65, 0, 200, 500], 64, 64, 64, True),
     "many_heads_128": ([333, 65, 0, 200, 500], [333, 65, 0, 200, 500], 64, 16, 128, True),
@@ -140,33 +159,34 @@ def test_prompt_views(dh):
 
 @pytest.mark.parametrize("dh", [64, 128])
 @pytest.mark.parametrize("value", [float("inf"), float("-inf"), float("nan")])
-@pytest.mark.parametrize("H,Hk", [(2, 1), (64, 64)])
-def test_prompt_what_is_not_seen_does_not_matter(dh, value, H, Hk):
+@pytest.mark.parametrize("H,Hk,lens", [(2, 1, [100, 90]), (64, 64, [100, 90]), (2, 1, [300, 250])])
+def test_prompt_what_is_not_seen_does_not_matter(dh, value, H, Hk, lens):
     """A key (a query) that is not finite touches only the queries (the keys) of its own pairs."""
-    lens, at = [100, 90], 70
+    at = 70
     Q, K, V, dY = prompt_inputs(lens, lens, H, Hk, dh, seed=21)
     clean = want_prompt(lens, lens, True, Q, K, V, dY)
     K2, V2 = K.clone(), V.clone()
     K2[at, :, 3] = value
     V2[at, :, 5] = value
     out = run_prompt(lens, lens, True, *(t.cuda() for t in (Q, K2, V2, dY)))
-    other = np.r_[0:at, 100:190]                                  # queries in front of the key, and the other sequence
+    T = sum(lens)
+    other = np.r_[0:at, lens[0]:T]                                # queries in front of the key, and the other sequence
     for name in ("Y", "dQ"):
         ref.check(name, ref.f64(out[name])[other], *(x[other] for x in clean[name]))
     ref.check("lse", ref.f64(out["lse"])[:, other], *(x[:, other] for x in clean["lse"]))
-    assert not torch.isfinite(out["Y"][at:100].float()).all(-1).any()
+    assert not torch.isfinite(out["Y"][at:lens[0]].float()).all(-1).any()
     for name in ("dK", "dV"):
-        ref.check(name, ref.f64(out[name])[100:190], *(x[100:190] for x in clean[name]))
+        ref.check(name, ref.f64(out[name])[lens[0]:T], *(x[lens[0]:T] for x in clean[name]))
     # and a query: its gradients go to the keys that it sees
     Q2, dY2, q_at = Q.clone(), dY.clone(), 40
     Q2[q_at, :, 2] = value
     dY2[q_at, :, 7] = value
     out = run_prompt(lens, lens, True, *(t.cuda() for t in (Q2, K, V, dY2)))
-    other = np.r_[q_at + 1:190]
+    other = np.r_[q_at + 1:T]
     for name in ("dK", "dV"):
         ref.check(name, ref.f64(out[name])[other], *(x[other] for x in clean[name]))
         assert not np.isfinite(ref.f64(out[name])[:q_at + 1]).all(-1).any(), name
-    other = np.r_[0:q_at, q_at + 1:190]
+    other = np.r_[0:q_at, q_at + 1:T]
     for name in ("Y", "dQ"):
         ref.check(name, ref.f64(out[name])[other], *(x[other] for x in clean[name]))
 
