@@ -63,14 +63,17 @@ inline int coarse_tiles(int64_t workgroups, int on_a_cu) {
   return rounds < 1 ? 0 : 63 - __builtin_clzll(rounds);
 }
 
-// Whether the 128 rows of a workgroup are dealt to four, whose wavefronts share what passes through LDS (`through` rows of B sequences)
-// instead of owning 32 rows each: where the four fit onto the chip at once and there is enough to share.  us, 128 rows and 32.
-// Forward: 8 heads of 128, 256 tokens 10.8 and 10.3, 512 14.3 and 12.1; 24 heads of 64, 384 (72 workgroups) 10.6 and 14.2; 2 heads, 4000 42 and 23.
-// Query side of the gradients: 12 heads of 64, 160 11.5 and 12.2, 256 14.1 and 12.6, 512 20.7 and 14.0; 24 heads, 384 15.7 and 20.6;
-// 2 heads, 4000 106 and 32.  Key side: 12 heads of 64, 77 10.5 and 11.8, 160 13.4 and 12.1, 512 24.5 and 14.3; 24 heads, 384
-// 18.2 and 20.3; 32 heads of 64 on 8, 512 61 and 23, of 128 on 8 63 and 37, 1024 115 and 64.
+// Wavefronts of a workgroup that own 32 rows each: four, or, where there are so few workgroups (of four) that twice or four times as many fit
+// onto the chip at once, two or one; four or eight groups of them then share what passes through LDS, if that is enough (`through` rows of B
+// sequences).  us, four (in the forward with two groups) and fewer owners.  Forward: 8 heads of 128, 256 tokens 10.8 and 10.3, 512 14.3 and
+// 12.1; 2 heads of 64, 4000 42 and 23, 8 heads, 2000 (125 workgroups) 25.5 and 19.3.  Query side of the gradients: 12 heads of 64,
+// 160 11.5 and 12.2, 256 14.1 and 12.6, 512 20.7 and 14.0, 1024 28 and 17; 2 heads, 4000 106 and 32.  Key side: 12 heads of 64, 77 10.5
+// and 11.8, 160 13.4 and 12.1, 512 24.5 and 14.3, 1024 33 and 18.5; 32 heads of 64 on 8, 512 61 and 23, of 128 on 8 63 and 37, two of
+// 1000 117 and 77.  One owner and two: 24 heads of 64, 384 (72 workgroups) query side 20.6 and 12.9, key side 20.3 and 13.0.
 constexpr int kFewTiles = 64;
-inline bool split_rows(int64_t workgroups, int64_t through, int B) { return workgroups <= kFewTiles && through >= 192 * (int64_t)B; }
+inline int row_owners(int64_t workgroups, int64_t through, int B) {
+  return workgroups > 2 * kFewTiles || through < 192 * (int64_t)B ? 4 : workgroups > kFewTiles ? 2 : 1;
+}
 
 // ---- device side
 

@@ -2,12 +2,13 @@
 //
 // A workgroup of four wavefronts owns 128 query rows: 128 / HW positions of one sequence times HW heads that
 // share a key head (HW: 4, 2 or 1, as divides the group).  A wavefront owns 32 of them.  Where there is less to do than the chip has
-// room for, two such groups share the keys, or four or eight wavefronts the keys of 32 rows.  Keys and values pass through LDS in
+// room for, two such groups share the keys, or four or eight groups of two or one those of 64 or 32 rows.  Keys and values pass through LDS in
 // tiles of 64 (32 so), copied asynchronously one tile ahead.  Scores are formed transposed, S^T = K Q^T, so that a lane holds 16
 // scores of ONE query and half of them are what the second product's operand wants of it: P stays in registers, and
 // maximum, sum and rescaling of a query are one lane's (two halves of a row meet in one lane swap).  O^T = V^T P^T takes V out of LDS
 // through the transposing read.  One pass over the keys: running maximum m and sum l, p = 2^(c s - m) with c = scale log2 e; the
 // accumulators are rescaled only when a maximum rises by more than 2^8 (p stays below 256, and the sums are fp32).
+#include <algorithm>
 #include <type_traits>
 
 #include "attn_common.hpp"
@@ -55,11 +56,11 @@ __device__ __forceinline__ void slow_row(const char* q, const char* k, int64_t k
   if (lse && lane == 0) *lse = (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
-// A workgroup: GROUPS groups of OWNERS wavefronts (four or one), which go through every GROUPS-th tile of 32 KT keys for the same queries.
+// A workgroup: GROUPS groups of OWNERS wavefronts (four, two or one), which go through every GROUPS-th tile of 32 KT keys for the same queries.
 template <int DH, int OWNERS, int GROUPS>
 struct FwdSizes {
   static constexpr int KT = OWNERS == 4 ? 2 : 1, TILE_KEYS = 32 * KT, TILE_BYTES = TILE_KEYS * DH * 2, RING = 4 * TILE_BYTES;   // K, V, twice
-  static constexpr int SHIFT = OWNERS == 4 ? 7 : 5, PART = DH * 128 + 512;   // 1 << SHIFT: rows; a wavefront's sums
+  static constexpr int SHIFT = OWNERS == 4 ? 7 : OWNERS == 2 ? 6 : 5, PART = DH * 128 + 512;   // 1 << SHIFT: rows; a wavefront's sums
   static constexpr int RINGS = GROUPS * RING, PARTS = (GROUPS - 1) * OWNERS * PART, SMEM = RINGS > PARTS ? RINGS : PARTS;
   static_assert(SMEM <= 160 * 1024, "a CU's LDS");
 };
@@ -272,7 +273,7 @@ hipError_t launch_fwd(FwdArgs a, const spt_attn_shape_t& s, hipStream_t st) {
   const auto kernel = prompt_fwd_kernel<DH, OWNERS, GROUPS>;
   static std::atomic<uint64_t> done{0};
   if (const hipError_t e = allow_smem(reinterpret_cast<const void*>(kernel), Sizes::SMEM, done); e != hipSuccess) return e;
-  if (OWNERS == 1) a.hshift = 0;
+  a.hshift = std::min(a.hshift, Sizes::SHIFT - 5);
   const int heads = a.G >> a.hshift, tiles = s.Tq >> (Sizes::SHIFT - a.hshift);
   a.coarse = coarse_tiles((int64_t)tiles * heads * s.Hk, DH == 128 ? 2 : 4);
   hipLaunchKernelGGL(kernel, dim3(head_item_grid(s.Hk, (tiles + s.B) * heads)), dim3(64 * OWNERS * GROUPS), Sizes::SMEM, st, a);   // (so many tiles at most)
@@ -321,8 +322,8 @@ extern "C" int spt_attn_prompt_fwd(const spt_attn_shape_t* shape, const void* Q,
   ScopedKernelTimer timer(kSlotAttnFwd, st);
   const auto launch = [&](auto dh) {
     constexpr int DH = decltype(dh)::value;
-    const int64_t tiles = (int64_t)(s.Tq >> (7 - a.hshift)) * (s.H >> a.hshift);
-    if (split_rows(tiles, s.Tk, s.B)) return launch_fwd<DH, 1, DH == 128 ? 4 : 8>(a, s, st);
+    const int owners = row_owners((int64_t)(s.Tq >> (7 - a.hshift)) * (s.H >> a.hshift), s.Tk, s.B);
+    if (owners < 4) return owners == 2 ? launch_fwd<DH, 2, 4>(a, s, st) : launch_fwd<DH, 1, DH == 128 ? 4 : 8>(a, s, st);
     return two_groups(s, a.hshift) ? launch_fwd<DH, 4, 2>(a, s, st) : launch_fwd<DH, 4, 1>(a, s, st);
   };
   const hipError_t e = s.dh == 128 ? launch(std::integral_constant<int, 128>()) : launch(std::integral_constant<int, 64>());

@@ -10,8 +10,10 @@
 //   prompt_bwd_kv_kernel  a wavefront owns 32 keys of a key head, the queries of all heads of its group pass through LDS in tiles
 //                         of 32, heads outermost, so a gradient is summed in one fixed order: S and dP with the key side in
 //                         registers, dV^T += dY^T P, dK^T += Q^T dS.
-// Where there is little to do, four or eight wavefronts share what passes through LDS for the same 32 rows, and their sums are added in order.
+// Where there is little to do, four or eight groups of wavefronts share what passes through LDS for the same 32 or 64 rows, and their sums are
+// added in order.
 // S and dP are formed in both: the alternative, keeping dS or partial dQ in memory, moves as many bytes as it saves time.
+#include <algorithm>
 #include <type_traits>
 
 #include "attn_common.hpp"
@@ -94,7 +96,7 @@ __device__ __forceinline__ void slow_dq_row(const BwdArgs& a, const char* q, con
 // tile for the same rows.
 template <int DH, int OWNERS, int GROUPS>
 struct BwdSizes {
-  static constexpr int TILE_BYTES = kTile * DH * 2, SHIFT = OWNERS == 4 ? 7 : 5, THREADS = 64 * OWNERS * GROUPS;   // 1 << SHIFT: rows
+  static constexpr int TILE_BYTES = kTile * DH * 2, SHIFT = OWNERS == 4 ? 7 : OWNERS == 2 ? 6 : 5, THREADS = 64 * OWNERS * GROUPS;   // 1 << SHIFT: rows
   // 128-wide heads: a row operand of the wavefront's own stays in LDS, or two wavefronts would not fit into a SIMD's registers
   static constexpr bool OWN = DH == 128;
   static constexpr int OWN_BYTES = OWN ? OWNERS * TILE_BYTES : 0;
@@ -138,7 +140,7 @@ __device__ __forceinline__ void add_groups(f32x16* sum, char* smem, int wave, in
 }
 
 template <int DH, int OWNERS, int GROUPS, bool EXACT>
-__global__ __launch_bounds__((64 * OWNERS * GROUPS), (OWNERS == 1 && DH == 128 ? 1 : 2)) void prompt_bwd_q_kernel(const BwdArgs a) {
+__global__ __launch_bounds__((64 * OWNERS * GROUPS), 2) void prompt_bwd_q_kernel(const BwdArgs a) {
   typedef BwdSizes<DH, OWNERS, GROUPS> Sizes;
   constexpr int KS = DH / 16, DT = DH / 32, TILE_BYTES = Sizes::TILE_BYTES;
   constexpr bool OWN = Sizes::OWN;
@@ -349,7 +351,7 @@ __device__ __forceinline__ void slow_dkv_row(const BwdArgs& a, const SeqRows& sq
 }
 
 template <int DH, int OWNERS, int GROUPS, bool EXACT>
-__global__ __launch_bounds__((64 * OWNERS * GROUPS), (OWNERS == 1 && DH == 128 ? 1 : 2)) void prompt_bwd_kv_kernel(const BwdArgs a) {
+__global__ __launch_bounds__((64 * OWNERS * GROUPS), 2) void prompt_bwd_kv_kernel(const BwdArgs a) {
   typedef BwdSizes<DH, OWNERS, GROUPS> Sizes;
   constexpr int KS = DH / 16, DT = DH / 32, TILE_BYTES = Sizes::TILE_BYTES, OWN_KEYS = kTile * OWNERS;
   constexpr bool OWN = Sizes::OWN;
@@ -571,7 +573,7 @@ hipError_t launch_q(BwdArgs a, const spt_attn_shape_t& s, hipStream_t st) {
   const auto kernel = prompt_bwd_q_kernel<DH, OWNERS, GROUPS, EXACT>;
   static std::atomic<uint64_t> done{0};
   if (const hipError_t e = allow_smem(reinterpret_cast<const void*>(kernel), Sizes::Q_SMEM, done); e != hipSuccess) return e;
-  if (OWNERS == 1) a.hshift = 0;
+  a.hshift = std::min(a.hshift, Sizes::SHIFT - 5);
   const int heads = a.G >> a.hshift, tiles = s.Tq >> (Sizes::SHIFT - a.hshift);
   a.coarse = coarse_tiles((int64_t)tiles * heads * s.Hk, DH == 128 ? 2 : 3);
   hipLaunchKernelGGL(kernel, dim3(head_item_grid(s.Hk, (tiles + s.B) * heads)), dim3(64 * OWNERS * GROUPS), Sizes::Q_SMEM, st, a);
@@ -625,18 +627,22 @@ extern "C" int spt_attn_prompt_bwd(const spt_attn_shape_t* shape, const void* Q,
   a.c = s.scale * kLog2e;
   const int64_t q_tiles = (int64_t)(s.Tq >> (7 - a.hshift)) * (s.H >> a.hshift), kv_tiles = (int64_t)(s.Tk >> 7) * s.Hk;
   const bool few = (int64_t)s.Tq * a.G <= (int64_t)kFewRows * s.B || q_tiles <= kFewTiles;
-  const bool split_q = split_rows(q_tiles, s.Tk, s.B), split_kv = split_rows(kv_tiles, (int64_t)s.Tq * a.G, s.B);
+  const int q_owners = row_owners(q_tiles, s.Tk, s.B), kv_owners = row_owners(kv_tiles, (int64_t)s.Tq * a.G, s.B);
   const hipStream_t st = static_cast<hipStream_t>(stream);
   const auto launches = [&](auto dh, auto exact) {
-    constexpr int DH = decltype(dh)::value, SPLIT = DH == 128 ? 4 : 8;
+    constexpr int DH = decltype(dh)::value, ONES = DH == 128 ? 4 : 8;
     constexpr bool EXACT = decltype(exact)::value;
     {
       ScopedKernelTimer timer(kSlotAttnBwdQ, st);
-      if (const hipError_t e = split_q ? launch_q<DH, 1, SPLIT, true>(a, s, st)   // (so few are exact)
-                                        : launch_q<DH, 4, 1, EXACT>(a, s, st); e != hipSuccess) return e;
+      const hipError_t e = q_owners == 4   ? launch_q<DH, 4, 1, EXACT>(a, s, st)
+                           : q_owners == 2 ? launch_q<DH, 2, 4, EXACT>(a, s, st)
+                                           : launch_q<DH, 1, ONES, true>(a, s, st);   // (so few are exact)
+      if (e != hipSuccess) return e;
     }
     ScopedKernelTimer timer(kSlotAttnBwdKV, st);
-    return split_kv ? launch_kv<DH, 1, SPLIT, EXACT>(a, s, st) : launch_kv<DH, 4, DH == 128 ? 2 : 1, EXACT>(a, s, st);
+    return kv_owners == 4   ? launch_kv<DH, 4, DH == 128 ? 2 : 1, EXACT>(a, s, st)
+           : kv_owners == 2 ? launch_kv<DH, 2, 4, EXACT>(a, s, st)
+                            : launch_kv<DH, 1, ONES, EXACT>(a, s, st);
   };
   const auto of = [&](auto dh) { return few ? launches(dh, std::true_type()) : launches(dh, std::false_type()); };
   const hipError_t e = s.dh == 128 ? of(std::integral_constant<int, 128>()) : of(std::integral_constant<int, 64>());

@@ -90,6 +90,12 @@ FEW = {   # few workgroups with much to read: rows in 32s, or on one side only
     "one_key_head_full": ([129, 400], [400, 129], 6, 1, False),
     "part_of_a_prompt": ([40, 1], [1000, 700], 4, 2, True),
     "more_queries": ([700, 31], [50, 300], 3, 3, True),
+    "rows_in_64s": ([300, 0, 451], [300, 0, 451], 16, 16, True),
+    "rows_in_64s_full": ([300, 1, 451], [290, 0, 461], 16, 16, False),
+    "rows_in_64s_groups_of_4": ([300, 0, 451], [300, 0, 451], 16, 4, True),
+    "rows_in_64s_groups_of_2": ([300, 33, 420], [300, 33, 420], 16, 8, True),
+    "keys_in_64s": ([300, 33, 420], [300, 33, 420], 32, 16, True),
+    "keys_in_64s_full": ([400, 352], [400, 352], 32, 16, False),
 }
 
 
@@ -159,7 +165,7 @@ def test_prompt_views(dh):
 
 @pytest.mark.parametrize("dh", [64, 128])
 @pytest.mark.parametrize("value", [float("inf"), float("-inf"), float("nan")])
-@pytest.mark.parametrize("H,Hk,lens", [(2, 1, [100, 90]), (64, 64, [100, 90]), (2, 1, [300, 250])])
+@pytest.mark.parametrize("H,Hk,lens", [(2, 1, [100, 90]), (64, 64, [100, 90]), (2, 1, [300, 250]), (16, 16, [300, 250])])
 def test_prompt_what_is_not_seen_does_not_matter(dh, value, H, Hk, lens):
     """A key (a query) that is not finite touches only the queries (the keys) of its own pairs."""
     at = 70
