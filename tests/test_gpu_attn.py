@@ -116,6 +116,7 @@ LARGE = {   # more workgroups than are resident at once; gradients summed over m
     "twelve_key_heads": ([400, 95, 33], [400, 95, 33], 24, 12, 128, True),
     "rounds_64": ([333, 65, 0, 200, 500], [333, 65, 0, 200, 500], 256, 256, 64, True),
     "rounds_128": ([300, 0, 200, 77], [300, 0, 410, 77], 256, 256, 128, True),
+    "most_sequences": ([(5 * i) % 3 for i in range(4096)], [(5 * i) % 3 for i in range(4096)], 4, 2, 64, True),
     "many_sequences": ([(7 * i) % 61 for i in range(150)], [(7 * i) % 61 + (5 * i) % 23 for i in range(150)], 128, 64, 64, True),
 }
 
@@ -213,11 +214,12 @@ def test_prompt_gradients_are_those_of_differences():
         assert abs(got - slope) <= (bounds[name][1] * np.abs(way)).sum() + 1e-5 * abs(slope) + 1e-4, (name, got, slope)
 
 
-def test_prompt_same_results_again_on_another_stream_and_in_a_graph():
-    lens, H, Hk, dh = [300, 17, 0, 129], 8, 2, 128
+@pytest.mark.parametrize("lens,H,Hk,dh", [([300, 17, 0, 129], 8, 2, 128), ([333, 65, 0, 500], 64, 64, 64), ([400, 300], 2, 1, 64),
+                                          ([300, 0, 451], 16, 16, 128)])
+def test_prompt_same_results_again_on_another_stream_and_in_a_graph(lens, H, Hk, dh):
     Q, K, V, dY = (t.cuda() for t in prompt_inputs(lens, lens, H, Hk, dh, seed=41))
     first = run_prompt(lens, lens, True, Q, K, V, dY)
-    shape = attn.make_shape(4, Q.shape[0], K.shape[0], H, Hk, dh)
+    shape = attn.make_shape(len(lens), Q.shape[0], K.shape[0], H, Hk, dh)
     cu = ref.sums(lens).cuda()
     n = sum(lens)
     ws = attn.alloc_prompt_workspace(shape)
@@ -448,6 +450,7 @@ DECODES = {
     "one_long": ([20011], 8, 2, 128, 64),
     "long_and_short": ([9000, 1, 0, 5, 2500], 4, 4, 64, 256),
     "many": ([(37 * n) % 130 for n in range(150)], 2, 1, 64, 16),
+    "thousands": ([(7 * n) % 41 for n in range(3000)], 2, 2, 64, 16),
 }
 
 
@@ -463,19 +466,21 @@ def test_decode(fmt, name, wide):
 
 
 @pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("width", [17, 100])
 @pytest.mark.parametrize("std,scale", [(8.0, None), (1.0, 3.0), (1e-30, None), (1e30, 1e-30)])
-def test_decode_sharp_and_flat(fmt, std, scale):
+def test_decode_sharp_and_flat(fmt, width, std, scale):
     lens = [513, 40]
-    shape, cache, table, Q, K, V = decode_inputs(fmt, lens, 4, 1, 128, 32, seed=7, std=std)
+    shape, cache, table, Q, K, V = decode_inputs(fmt, lens, 4, 1, 128, 32, seed=7, std=std, width=width)
     Y = attn.decode(shape, Q.cuda(), cache, table, ints(lens), scale=scale)
     ref.check("Y", Y, *want_decode(Q, K, V, lens, None if scale is None else float(np.float32(scale))))
 
 
 @pytest.mark.parametrize("fmt", FORMATS)
-def test_decode_lengths_and_pages_that_are_not_there(fmt):
+@pytest.mark.parametrize("width", [7, 200])
+def test_decode_lengths_and_pages_that_are_not_there(fmt, width):
     """Lengths below 0 and behind the table; tokens whose page is no page of the pool are left out."""
     lens, page = [100, 40, 64], 16
-    shape, cache, table, Q, K, V = decode_inputs(fmt, lens, 4, 2, 64, page, width=7)
+    shape, cache, table, Q, K, V = decode_inputs(fmt, lens, 4, 2, 64, page, width=width)
     Y = attn.decode(shape, Q.cuda(), cache, table, ints([-3, 40, 1000000]))
     assert (Y[0] == 0).all()
     keep = want_decode(Q, K, V, lens)
@@ -488,8 +493,9 @@ def test_decode_lengths_and_pages_that_are_not_there(fmt):
 
 
 @pytest.mark.parametrize("fmt", FORMATS)
-def test_decode_same_results_again_views_and_graph(fmt):
-    lens = [1500, 3, 0, 260]
+@pytest.mark.parametrize("longest", [1500, 500])
+def test_decode_same_results_again_views_and_graph(fmt, longest):
+    lens = [longest, 3, 0, 260]
     shape, cache, table, Q, K, V = decode_inputs(fmt, lens, 8, 2, 128, 64, seed=11)
     n, q = ints(lens), Q.cuda()
     first = attn.decode(shape, q, cache, table, n)
@@ -504,7 +510,7 @@ def test_decode_same_results_again_views_and_graph(fmt):
     side = torch.cuda.Stream()
     with torch.cuda.graph(graph, stream=side):
         attn.decode(shape, q, cache, table, n, ws=ws, Y=out)
-    for changed in (lens, [1499, 2, 70, 1], lens):
+    for changed in (lens, [longest - 1, 2, 70, 1], lens):
         m = [min(a, b) for a, b in zip(changed, lens)]
         n.copy_(ints(m))
         out.zero_()
@@ -533,7 +539,45 @@ def test_pages_behind_32_bits(fmt):
     ref.check("Y", attn.decode(shape, Q.cuda(), cache, table, ints(lens)), *want_decode(Q, held(K, fmt), held(V, fmt), lens))
 
 
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("width", [20, 200])
+def test_decode_a_head_that_is_not_finite(fmt, width):
+    """NaN in one query touches the output of that query alone."""
+    lens = [300, 77]
+    shape, cache, table, Q, K, V = decode_inputs(fmt, lens, 8, 2, 64, 16, seed=13, width=width)
+    first = attn.decode(shape, Q.cuda(), cache, table, ints(lens))
+    bad = Q.clone()
+    bad[0, 5, 7] = float("nan")
+    Y = attn.decode(shape, bad.cuda(), cache, table, ints(lens))
+    assert torch.isnan(Y[0, 5]).all()
+    Y[0, 5] = first[0, 5]
+    assert torch.equal(Y, first)
+
+
 # ---- together
+
+def test_calls_at_once():
+    """Calls on two streams, each with a workspace of its own, do not see one another."""
+    lens, H, Hk, dh = [300, 17, 129], 8, 2, 128
+    inputs = [tuple(t.cuda() for t in prompt_inputs(lens, lens, H, Hk, dh, seed=80 + n)) for n in range(2)]
+    decodes = [decode_inputs("e4m3", [2000, 30, 700], H, Hk, dh, 64, seed=90 + n, width=40) for n in range(2)]
+    n = ints([2000, 30, 700])
+    alone = [(run_prompt(lens, lens, True, *x), attn.decode(d[0], d[3].cuda(), d[1], d[2], n)) for x, d in zip(inputs, decodes)]
+    queries = [d[3].cuda() for d in decodes]
+    streams, got = [torch.cuda.Stream() for _ in range(2)], [[], []]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for k, stream in enumerate(streams):
+            with torch.cuda.stream(stream):
+                got[k].append((run_prompt(lens, lens, True, *inputs[k]), attn.decode(decodes[k][0], queries[k], decodes[k][1], decodes[k][2], n)))
+    torch.cuda.synchronize()
+    for k in range(2):
+        for out, Y in got[k]:
+            assert torch.equal(Y, alone[k][1])
+            for x in out:
+                a, b = (out[x][:, :sum(lens)], alone[k][0][x][:, :sum(lens)]) if x == "lse" else (out[x][:sum(lens)], alone[k][0][x][:sum(lens)])
+                assert torch.equal(a, b), x
+
 
 @pytest.mark.parametrize("fmt", FORMATS)
 @pytest.mark.parametrize("H,Hk,dh,page", [(8, 2, 128, 16), (4, 4, 64, 64)])
