@@ -78,11 +78,11 @@ __global__ __launch_bounds__(256) void cache_write_kernel(const RowArgs a) {
     const bool v = n >= a.c.Hk;
     const int hk = v ? n - a.c.Hk : n;
     const AttnRows& src = v ? a.V : a.K;
-    const u32x4 x = *reinterpret_cast<const u32x4*>(src.p + r * src.row + hk * src.head + piece * 16);
+    const u32x4 x = stream_in<u32x4>(src.p + r * src.row + hk * src.head + piece * 16);
     const int64_t at = place + ((int64_t)hk << a.c.page_shift);
     char* dst = v ? a.c.Vc : a.c.Kc;
     if (!E4M3) {
-      *reinterpret_cast<u32x4*>(dst + at * (DH * 2) + piece * 16) = x;
+      stream_out(dst + at * (DH * 2) + piece * 16, x);
       continue;
     }
     uint32_t top = 0;
@@ -103,7 +103,7 @@ __global__ __launch_bounds__(256) void cache_write_kernel(const RowArgs a) {
     for (int e = 0; e < 8; ++e)
       f[e] = (__float_as_uint(f[e]) & 0x7F800000u) == 0x7F800000u ? __builtin_nanf("")
                                                                   : __builtin_amdgcn_fmed3f(__builtin_ldexpf(f[e], 127 - byte), -most, most);
-    *reinterpret_cast<uint2*>(dst + at * DH + piece * 8) = make_uint2(code4(f), code4(f + 4));
+    stream_out(dst + at * DH + piece * 8, u32x2{code4(f), code4(f + 4)});
     if (piece == 0) (v ? a.c.vs : a.c.ks)[at] = (uint8_t)byte;
   }
 }
@@ -139,15 +139,15 @@ __global__ __launch_bounds__(256) void cache_read_kernel(const RowArgs a) {
     u32x4 x = {0, 0, 0, 0};
     if (place >= 0) {
       if (!E4M3) {
-        x = *reinterpret_cast<const u32x4*>(src + at * (DH * 2) + piece * 16);
+        x = stream_in<u32x4>(src + at * (DH * 2) + piece * 16);
       } else {
-        const uint2 w = *reinterpret_cast<const uint2*>(src + at * DH + piece * 8);
+        const u32x2 w = stream_in<u32x2>(src + at * DH + piece * 8);
         const int byte = (v ? a.c.vs : a.c.ks)[at];
-        const uint2 lo = held4(w.x, byte), hi = held4(w.y, byte);
+        const uint2 lo = held4(w[0], byte), hi = held4(w[1], byte);
         x = u32x4{lo.x, lo.y, hi.x, hi.y};
       }
     }
-    *reinterpret_cast<u32x4*>(to.p + r * to.row + hk * to.head + piece * 16) = x;
+    stream_out(to.p + r * to.row + hk * to.head + piece * 16, x);
   }
 }
 

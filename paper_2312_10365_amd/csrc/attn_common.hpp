@@ -185,6 +185,14 @@ __device__ __forceinline__ void dma16_at(const void* base, uint32_t off, uint32_
 }
 __device__ __forceinline__ uint32_t lds_addr(const void* p) { return __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)p); }
 
+// 16 (8) bytes of whole lines that this launch does not read again: not kept in L2, which the end of a launch would wait to have written
+// (rows written to a cache and read back, 102 MB each way: 52.5 us kept, 47.3 so; stores that leave lines in parts lose by it).
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+template <class T>
+__device__ __forceinline__ void stream_out(char* p, T v) { __builtin_nontemporal_store(v, reinterpret_cast<T*>(p)); }
+template <class T>
+__device__ __forceinline__ T stream_in(const char* p) { return __builtin_nontemporal_load(reinterpret_cast<const T*>(p)); }
+
 // LDS by its 32-bit address.
 template <class T>
 __device__ __forceinline__ T lds_read(uint32_t at) {
@@ -258,13 +266,20 @@ __device__ __forceinline__ void put_dims(char* tile, int r, int c, bf16x8 lo, bf
   *reinterpret_cast<bf16x8*>(tile + (at ^ 16u)) = hi;
 }
 template <int DH>
-__device__ __forceinline__ void store_rows(const char* tile, char* x, int64_t row, int n, int lane) {
+__device__ __forceinline__ void store_rows(const char* tile, char* x, int64_t row, int n, int lane, bool stream = false) {
   constexpr int CHUNKS = DH / 8, ROWS = 64 / CHUNKS;
 #pragma unroll
   for (int u = 0; u < 32 / ROWS; ++u) {
     const int r = u * ROWS + lane / CHUNKS;
     const u32x4 v = *reinterpret_cast<const u32x4*>(tile + u * 1024 + lane * 16);
-    if (r < n) *reinterpret_cast<u32x4*>(x + r * row + (((uint32_t)lane % CHUNKS) ^ row_swizzle<DH>(r)) * 16) = v;
+    char* to = x + r * row + (((uint32_t)lane % CHUNKS) ^ row_swizzle<DH>(r)) * 16;
+    if (r < n && stream) {
+      asm volatile("");                                    // (or the compiler makes one store of the two, and keeps it in L2)
+      stream_out(to, v);
+      asm volatile("");
+    } else if (r < n) {
+      *reinterpret_cast<u32x4*>(to) = v;
+    }
   }
 }
 

@@ -254,7 +254,8 @@ __global__ __launch_bounds__((64 * OWNERS * GROUPS), 2) void prompt_fwd_kernel(c
     put_dims<DH>(smem + out, i, 4 * d + 2 * h, pack8(v), pack8(v + 8));
   }
   wave_lds_fence();
-  store_rows<DH>(smem + out, a.Y.p + (int64_t)(sq.first + i0) * a.Y.row + (int64_t)head * a.Y.head, a.Y.row, nq - i0, lane);
+  store_rows<DH>(smem + out, a.Y.p + (int64_t)(sq.first + i0) * a.Y.row + (int64_t)head * a.Y.head, a.Y.row, nq - i0, lane,
+                 !a.lse);   // (a backward that follows reads Y: 16 sequences of 512, 32 heads of 64 178 us kept, 180 streamed; 16 prompts of 33 to 2000, 32 heads of 128 on 8, without one 109.7 and 107.2)
 }
 
 // Two groups of wavefronts a workgroup where the chip would not be full: with no more workgroups than are resident at once (two on a CU at
