@@ -327,7 +327,9 @@ struct DecodeState {
   }
 };
 
-// Asynchronous copies of unit t of a sequence into a stage; returns which of its 32 tokens are there.
+// Asynchronous copies of unit t of a sequence into a stage; returns which of its 32 tokens are there.  Nobody reads a row again in the launch
+// (two sets of a group's heads do): kept in L2 48 sequences of 100 to 8000 tokens in 8 bits, 32 heads of 128 on 8, went in 45.8 us, 41.2 so,
+// six of 30000 to 32700 in 16 bits in 137 (5.6 TB/s) and 121 (6.4).
 template <int DH, bool E4M3>
 __device__ __forceinline__ uint32_t fetch_unit(const DecodeArgs& a, int hk, int t, int len, const int* page, uint32_t at, uint32_t exponents, int lane) {
   constexpr int RB = E4M3 ? DH : DH * 2, BYTES = kUnit * RB;
@@ -345,8 +347,8 @@ __device__ __forceinline__ uint32_t fetch_unit(const DecodeArgs& a, int hk, int 
     const int r = n * (1024 / RB) + lane / (RB / 16);        // row of the unit; those of a copy lie in one half
     const int half = n * (1024 / RB) / 16;
     const uint32_t off = (uint32_t)(r - 16 * half) * RB + (((uint32_t)lane % (RB / 16)) ^ chunk_swizzle<RB>(r)) * 16;
-    dma16_at(a.c.Kc + row[half] * RB, off, at + n * 1024);
-    dma16_at(a.c.Vc + row[half] * RB, off, at + BYTES + n * 1024);
+    dma16_once(a.c.Kc + row[half] * RB, off, at + n * 1024);
+    dma16_once(a.c.Vc + row[half] * RB, off, at + BYTES + n * 1024);
   }
   if (E4M3) {                                                // lanes 0-7: exponents of the keys, 8-15: of the values
     const int half = (lane >> 2) & 1;
@@ -729,9 +731,9 @@ hipError_t launch_items(const DecodeArgs& a, hipStream_t st) {
 }
 
 // Whether a table is so narrow that a wavefront of an item's workgroup has four units at most: then the launch of the joins costs more than
-// an even split gains.  us a call in a graph, stretches and items, 32 heads on 8 of 128: 32 sequences of 512 tokens 19.2 and 14.2, one of
-// them 8.8 and 8.5, 64 of 10 to 1000 in 8 bits 16.6 and 15.7, 16 of 1000 14.4 and 12.2; one sequence of 100, 32 heads of 64: 8.4 and 4.2.
-// Wider tables: one of 1024 in 16 bits (four wavefronts) 9.3 and 13.4, one of 2048 in 8 bits 9.4 and 16.9.
+// an even split gains.  us a call in a graph, stretches and items, 32 heads on 8 of 128: 32 sequences of 512 tokens 17.3 and 12.4, one of
+// them 8.8 and 8.5, 64 of 10 to 1000 in 8 bits 16.4 and 15.9, 16 of 1000 14.2 and 11.7, 4 of them 10.2 and 11.7; one sequence of 100, 32 heads
+// of 64: 8.3 and 4.2.  Wider tables: one of 1024 in 16 bits (four wavefronts) 9.4 and 13.6, one of 2048 in 8 bits 9.4 and 17.6.
 bool short_table(const spt_cache_shape_t& s) {
   const int waves = s.format == SPT_CACHE_BF16 && s.dh == 128 ? ItemTile<128, false>::WAVES : ItemTile<64, false>::WAVES;
   return (int64_t)s.max_pages * s.page <= 4 * kUnit * waves;

@@ -183,6 +183,10 @@ __device__ __forceinline__ uint32_t row_swizzle(int r) { return chunk_swizzle<DH
 __device__ __forceinline__ void dma16_at(const void* base, uint32_t off, uint32_t lds_base) {
   asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds_base), "v"(off), "s"(base) : "memory");
 }
+// The same for what a launch reads once: it does not stay in L2.
+__device__ __forceinline__ void dma16_once(const void* base, uint32_t off, uint32_t lds_base) {
+  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2 nt" ::"s"(lds_base), "v"(off), "s"(base) : "memory");
+}
 __device__ __forceinline__ uint32_t lds_addr(const void* p) { return __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)p); }
 
 // 16 (8) bytes of whole lines that this launch does not read again: not kept in L2, which the end of a launch would wait to have written
