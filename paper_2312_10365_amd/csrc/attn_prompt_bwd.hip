@@ -96,7 +96,7 @@ __device__ __forceinline__ void slow_dq_row(const BwdArgs& a, const char* q, con
 // tile for the same rows.
 template <int DH, int OWNERS, int GROUPS>
 struct BwdSizes {
-  static constexpr int TILE_BYTES = kTile * DH * 2, SHIFT = OWNERS == 4 ? 7 : OWNERS == 2 ? 6 : 5, THREADS = 64 * OWNERS * GROUPS;   // 1 << SHIFT: rows
+  static constexpr int TILE_BYTES = kTile * DH * 2, SHIFT = OWNERS == 8 ? 8 : OWNERS == 4 ? 7 : OWNERS == 2 ? 6 : 5, THREADS = 64 * OWNERS * GROUPS;   // 1 << SHIFT: rows
   // 128-wide heads: a row operand of the wavefront's own stays in LDS, or two wavefronts would not fit into a SIMD's registers
   static constexpr bool OWN = DH == 128;
   static constexpr int OWN_BYTES = OWN ? OWNERS * TILE_BYTES : 0;
@@ -567,6 +567,15 @@ __global__ __launch_bounds__((64 * OWNERS * GROUPS), 2) void prompt_bwd_kv_kerne
   }
 }
 
+// Key side, 128-wide heads: whether eight wavefronts own 256 keys, so that twice as many read a tile in LDS as of two groups of four, where
+// there are sequences that long and rounds enough of workgroups, which `causal` makes unequal.  us, two groups and eight owners: 32 heads,
+// 4 sequences of 2048 347 and 325, all keys seen 590 and 530; 20 of 512 (1280 workgroups) 192 and 180, 262 and 229; 32 heads on 8, one of
+// 8192 (256 workgroups), all seen 1984 and 1874, but causal 1059 and 1659; 24 of 33 to 2000 (750) 465 and 475; 40 of 100 to 300, all seen 94 and 118.
+// (64-wide heads: two wavefronts of a workgroup on every SIMD, where there is room for three.)
+bool eight_owners(const spt_attn_shape_t& s) {
+  return (int64_t)(s.Tk >> 8) * s.Hk >= (s.causal ? 1024 : 256) && s.Tk >= 256 * (int64_t)s.B;
+}
+
 template <int DH, int OWNERS, int GROUPS, bool EXACT>
 hipError_t launch_q(BwdArgs a, const spt_attn_shape_t& s, hipStream_t st) {
   typedef BwdSizes<DH, OWNERS, GROUPS> Sizes;
@@ -640,6 +649,9 @@ extern "C" int spt_attn_prompt_bwd(const spt_attn_shape_t* shape, const void* Q,
       if (e != hipSuccess) return e;
     }
     ScopedKernelTimer timer(kSlotAttnBwdKV, st);
+    if constexpr (DH == 128) {
+      if (eight_owners(s)) return launch_kv<DH, 8, 1, EXACT>(a, s, st);
+    }
     return kv_owners == 4   ? launch_kv<DH, 4, DH == 128 ? 2 : 1, EXACT>(a, s, st)
            : kv_owners == 2 ? launch_kv<DH, 2, 4, EXACT>(a, s, st)
                             : launch_kv<DH, 1, ONES, EXACT>(a, s, st);

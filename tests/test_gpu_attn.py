@@ -115,6 +115,8 @@ LARGE = {   # more workgroups than are resident at once; gradients summed over m
     "many_heads_part": ([130, 257, 64], [700, 300, 1], 48, 16, 128, True),
     "twelve_key_heads": ([400, 95, 33], [400, 95, 33], 24, 12, 128, True),
     "rounds_64": ([333, 65, 0, 200, 500], [333, 65, 0, 200, 500], 256, 256, 64, True),
+    "keys_in_256s": ([520, 700, 33, 290], [520, 700, 33, 290], 176, 176, 128, True),
+    "keys_in_256s_full": ([300, 0, 512, 200], [300, 1, 511, 255], 128, 64, 128, False),
     "rounds_128": ([300, 0, 200, 77], [300, 0, 410, 77], 256, 256, 128, True),
     "most_sequences": ([(5 * i) % 3 for i in range(4096)], [(5 * i) % 3 for i in range(4096)], 4, 2, 64, True),
     "many_sequences": ([(7 * i) % 61 for i in range(150)], [(7 * i) % 61 + (5 * i) % 23 for i in range(150)], 128, 64, 64, True),
@@ -164,10 +166,7 @@ def test_prompt_views(dh):
     assert torch.equal(a, attn.prompt_fwd(shape, q, one.contiguous(), v, cu, cu)[0])
 
 
-@pytest.mark.parametrize("dh", [64, 128])
-@pytest.mark.parametrize("value", [float("inf"), float("-inf"), float("nan")])
-@pytest.mark.parametrize("H,Hk,lens", [(2, 1, [100, 90]), (64, 64, [100, 90]), (2, 1, [300, 250]), (16, 16, [300, 250])])
-def test_prompt_what_is_not_seen_does_not_matter(dh, value, H, Hk, lens):
+not_seen_does_not_matter(dh, value, H, Hk, lens):
     """A key (a query) that is not finite touches only the queries (the keys) of its own pairs."""
     at = 70
     Q, K, V, dY = prompt_inputs(lens, lens, H, Hk, dh, seed=21)
@@ -196,6 +195,17 @@ def test_prompt_what_is_not_seen_does_not_matter(dh, value, H, Hk, lens):
     other = np.r_[0:q_at, q_at + 1:T]
     for name in ("Y", "dQ"):
         ref.check(name, ref.f64(out[name])[other], *(x[other] for x in clean[name]))
+
+
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("value", [float("inf"), float("-inf"), float("nan")])
+@pytest.mark.parametrize("H,Hk,lens", [(2, 1, [100, 90]), (64, 64, [100, 90]), (2, 1, [300, 250]), (16, 16, [300, 250])])
+def test_prompt_what_is_not_seen_does_not_matter(dh, value, H, Hk, lens):
+    check_not_seen(dh, value, H, Hk, lens)
+
+
+def test_prompt_what_is_not_seen_does_not_matter_keys_in_256s():
+    check_not_seen(128, float("nan"), 256, 256, [530, 520])
 
 
 def test_prompt_gradients_are_those_of_differences():
