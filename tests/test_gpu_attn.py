@@ -166,7 +166,7 @@ def test_prompt_views(dh):
     assert torch.equal(a, attn.prompt_fwd(shape, q, one.contiguous(), v, cu, cu)[0])
 
 
-not_seen_does_not_matter(dh, value, H, Hk, lens):
+def check_not_seen(dh, value, H, Hk, lens):
     """A key (a query) that is not finite touches only the queries (the keys) of its own pairs."""
     at = 70
     Q, K, V, dY = prompt_inputs(lens, lens, H, Hk, dh, seed=21)
