@@ -255,14 +255,15 @@ __global__ __launch_bounds__((64 * OWNERS * GROUPS), 2) void prompt_fwd_kernel(c
   }
   wave_lds_fence();
   store_rows<DH>(smem + out, a.Y.p + (int64_t)(sq.first + i0) * a.Y.row + (int64_t)head * a.Y.head, a.Y.row, nq - i0, lane,
-                 !a.lse);   // (a backward that follows reads Y: 16 sequences of 512, 32 heads of 64 178 us kept, 180 streamed; 16 prompts of 33 to 2000, 32 heads of 128 on 8, without one 109.7 and 107.2)
+                 !a.lse);   // (a backward that follows reads Y: 16 sequences of 512, 32 heads of 64 178 us kept, 180 streamed; without one, 16
+                            // prompts of 33 to 2000, 32 heads of 128 on 8, 109.7 and 107.2)
 }
 
-// Two groups of wavefronts a workgroup where the chip would not be full: with no more workgroups than are resident at once (two on a CU at
-// dh 128; at dh 64 four, of which three count) the one with the most keys is what the launch waits for.  us, one group and two, 32 heads on 8 of
-// 128: one sequence of 2048 56.6 and 49.2, 512 queries behind 4000 keys 98.7 and 75.7, four parts of 512 behind 700 to 5000 146 and 129;
-// of 4096 (twice as many as are resident) 154 and 158; four of 512, which have few tiles to share, 23.0 and 26.2, one of them 17.5 and 16.4; 12
-// heads of 64, one of 1000 21.2 and 17.1, of 8000 146 and 133; 32 heads of 64, four of 1024 (four workgroups on a CU) 33 and 37.
+// Two groups of four wavefronts a workgroup where the chip would not be full: with no more workgroups than are resident at once (two on a CU
+// at dh 128; at dh 64 four, of which three count) the one with the most keys is what the launch waits for.  us, one group and two, 32 heads on
+// 8 of 128: one sequence of 2048 56.6 and 49.2, four parts of 512 behind 700 to 5000 146 and 129; of 4096 (twice as many workgroups as are
+// resident) 154 and 158; four of 512, which have few tiles to share, 23.0 and 26.2; 12 heads of 64, one of 8000 146 and 133; 32 heads of 64,
+// four of 1024 (four workgroups on a CU) 33 and 37.
 bool two_groups(const spt_attn_shape_t& s, int hshift) {
   const int64_t workgroups = (int64_t)(s.Tq >> (7 - hshift)) * (s.H >> hshift), resident = 256 * (s.dh == 128 ? 2 : 3);
   return workgroups <= resident / 2 || (workgroups <= resident && s.Tk >= 1024 * (int64_t)s.B);
