@@ -59,7 +59,8 @@ int spt_attn_prompt_fwd(const spt_attn_shape_t* shape, const void* Q, const void
  * A query that sees no key has dq = 0, a key that no query sees dk = dv = 0; rows behind cu_q[B], cu_k[B] are left as they were.
  *   strides  host, or NULL: of Q, K, V, Y, dY, dQ, dK, dV: 16 numbers
  *   ws       spt_attn_prompt_workspace_bytes(shape) bytes, 256-byte aligned
- * P and dS are rounded to bf16 in front of their products. */
+ * In front of their products P is rounded to bf16, dS to bf16 or, where there are few rows, to the sum of two.  What the
+ * rounding of Y leaves in the sum of a row's dS, which is 0, is taken off D. */
 int spt_attn_prompt_bwd(const spt_attn_shape_t* shape, const void* Q, const void* K, const void* V,
                         const void* Y, const void* dY, const float* lse, const int64_t* strides,
                         const int32_t* cu_q, const int32_t* cu_k, void* dQ, void* dK, void* dV, void* ws,
