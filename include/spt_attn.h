@@ -35,7 +35,7 @@ typedef struct {
   int32_t H, Hk;  /* query heads (at most 65535; B H and Tq H / 128 together below 2^23), key heads */
   int32_t dh;     /* 64 or 128 */
   int32_t causal; /* 0 or 1 */
-  float scale;    /* logits are scale * q.k; positive and finite */
+  float scale;    /* logits are scale * q.k; positive, at most 2e38 */
 } spt_attn_shape_t;
 
 /* y_i = sum_j p_ij v_j, p_ij = exp(s_ij - lse_i), s_ij = scale q_i.k_j, lse_i = log sum_j exp(s_ij),
@@ -111,7 +111,7 @@ int spt_cache_read(const spt_cache_shape_t* shape, int32_t T, void* K, void* V, 
  * a score above -inf, gives zeros; lengths above max_pages * page count as that; tokens whose entry of table lies outside
  * 0 .. pages - 1 are left out.  What lies in a page behind the last token does not matter.
  *   Q, Y bf16 [B][H][dh];  strides host, or NULL for dense: of Q, Y: 4 numbers, as above
- *   lens int32 [B];  scale positive and finite
+ *   lens int32 [B];  scale positive, at most 2e38
  *   ws: spt_attn_decode_workspace_bytes(shape, H) bytes, 256-byte aligned
  * B * Hk * ceil(max_pages * page / 32) * ceil(H / Hk / 16) must be below 2^31, B * H below 2^23 - 16. */
 int spt_attn_decode(const spt_cache_shape_t* shape, int32_t H, float scale, const void* Q, const int64_t* strides,

@@ -789,7 +789,7 @@ extern "C" int spt_attn_decode(const spt_cache_shape_t* shape, int32_t H, float 
                                void* ws, size_t ws_bytes, void* stream) {
   int rc = check_decode(shape, H);
   if (rc != SPT_OK) return rc;
-  if (!isfinite(scale) || !(scale > 0.f)) return SPT_ERR_ARG;
+  if (!(scale > 0.f) || !(scale <= kMostScale)) return SPT_ERR_ARG;
   const spt_cache_shape_t& s = *shape;
   DecodeArgs a;
   if ((rc = attn_rows(&a.Q, Q, strides, s.B, H, s.dh, false)) != SPT_OK) return rc;

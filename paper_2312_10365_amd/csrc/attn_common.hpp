@@ -48,6 +48,7 @@ inline hipError_t allow_smem(const void* kernel, int smem, std::atomic<uint64_t>
   return e;
 }
 
+constexpr float kMostScale = 2e38f;                    // times log2 e it is finite
 constexpr int64_t kMostWorkgroups = (1 << 23) - 16;   // of up to 512 threads: a launch has fewer than 2^32
 
 int check_attn(const spt_attn_shape_t* s);   // attn_prompt.hip

@@ -290,7 +290,7 @@ int check_attn(const spt_attn_shape_t* s) {
   if (!s) return SPT_ERR_ARG;
   if (s->B < 1 || s->Tq < 1 || s->Tk < 1 || s->H < 1 || s->Hk < 1 || s->dh < 1 || s->H % s->Hk != 0) return SPT_ERR_ARG;
   if (s->causal != 0 && s->causal != 1) return SPT_ERR_ARG;
-  if (!isfinite(s->scale) || !(s->scale > 0.f)) return SPT_ERR_ARG;
+  if (!(s->scale > 0.f) || !(s->scale <= kMostScale)) return SPT_ERR_ARG;
   if ((s->dh != 64 && s->dh != 128) || s->B > 4096 || s->H > 65535) return SPT_ERR_UNSUPPORTED;
   const int shift = attn_heads_shift(s->H / s->Hk);   // (tiles of 128 rows of heads; of 128 keys)
   if (((int64_t)(s->Tq >> (7 - shift)) + s->B) * (s->H >> shift) > kMostWorkgroups) return SPT_ERR_UNSUPPORTED;

@@ -38,7 +38,7 @@ def bwd(shape, strides=None, ws=OK, ws_bytes=1 << 40, **other):
 
 @pytest.mark.parametrize("change,code", [
     (dict(B=0), ARG), (dict(Tq=0), ARG), (dict(Tk=0), ARG), (dict(H=0), ARG), (dict(Hk=0), ARG), (dict(Hk=3), ARG), (dict(dh=0), ARG),
-    (dict(causal=2), ARG), (dict(scale=0.0), ARG), (dict(scale=-1.0), ARG), (dict(scale=float("nan")), ARG), (dict(scale=float("inf")), ARG),
+    (dict(causal=2), ARG), (dict(scale=0.0), ARG), (dict(scale=-1.0), ARG), (dict(scale=float("nan")), ARG), (dict(scale=float("inf")), ARG), (dict(scale=3e38), ARG),
     (dict(dh=32), UNSUPPORTED), (dict(dh=96), UNSUPPORTED), (dict(B=4097), UNSUPPORTED), (dict(H=1 << 17, Hk=1), UNSUPPORTED),
     (dict(Tq=2 ** 31 - 1, H=64, Hk=1), UNSUPPORTED), (dict(Tk=2 ** 31 - 1, H=64, Hk=1), UNSUPPORTED)])
 def test_prompt_shapes(change, code):
@@ -117,7 +117,7 @@ def test_cache_pointers_and_strides():
 def test_decode_arguments():
     s, s8 = pool(), pool(dict(format=attn.CACHE_E4M3))
     assert decode(s, H=0) == ARG and decode(s, H=3) == ARG and decode(s, H=1 << 17) == UNSUPPORTED
-    for scale in (0.0, -1.0, float("nan"), float("inf")):
+    for scale in (0.0, -1.0, float("nan"), float("inf"), 3e38):
         assert decode(s, scale=scale) == ARG
     for name in ("Q", "Kc", "Vc", "table", "lens", "Y", "ws"):
         assert decode(s, **{name: None}) == ARG, name
