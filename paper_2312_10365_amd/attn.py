@@ -98,13 +98,15 @@ def alloc_decode_workspace(shape: CacheShape, H: int, device="cuda") -> torch.Te
 
 _BF16, _F32, _I32, _U8 = torch.bfloat16, torch.float32, torch.int32, torch.uint8
 _byref = ctypes.byref
+_current_device, _current_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
 
 
 def _gpu(t, name: str) -> int:
     """The GPU of a call's first tensor, which all others must be on."""
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+    dev = t.get_device() if isinstance(t, torch.Tensor) else -1
+    if dev < 0:
         raise ValueError(f"{name}: need a tensor on a GPU")
-    return t.get_device()
+    return dev
 
 
 def _dense(t, dtype, numel: int, dev: int, name: str):
@@ -140,11 +142,11 @@ def _strides(apart: list, *tensors):
 def _call(dev: int, name: str, *args):
     """Calls launch on the current device and its current stream: make it the tensors' device."""
     f = _functions.get(name) or _functions.setdefault(name, getattr(lib(), name))
-    if dev == torch._C._cuda_getDevice():
-        rc = f(*args, torch._C._cuda_getCurrentRawStream(dev))
+    if dev == _current_device():
+        rc = f(*args, _current_stream(dev))
     else:
         with torch.cuda.device(dev):
-            rc = f(*args, torch._C._cuda_getCurrentRawStream(dev))
+            rc = f(*args, _current_stream(dev))
     if rc != 0:
         raise spt.SptError(rc, name)
 
@@ -178,12 +180,12 @@ def prompt_bwd(shape: AttnShape, Q, K, V, Y, dY, lse, cu_q, cu_k, ws=None, dQ=No
     dQ, dK, dV = (torch.empty(n, dtype=_BF16, device=Q.device) if t is None else t for t, n in ((dQ, q), (dK, k), (dV, k)))
     if ws is None:
         ws = alloc_prompt_workspace(s, Q.device)
-    apart = []
+    apart, size = [], ws.numel()
     dq, dk, dv = _rows(dQ, q, dev, "dQ", apart), _rows(dK, k, dev, "dK", apart), _rows(dV, k, dev, "dV", apart)
     _call(dev, "spt_attn_prompt_bwd", _byref(s), _rows(Q, q, dev, "Q", apart), _rows(K, k, dev, "K", apart), _rows(V, k, dev, "V", apart),
           _rows(Y, q, dev, "Y", apart), _rows(dY, q, dev, "dY", apart), _dense(lse, _F32, H * Tq, dev, "lse"),
           _strides(apart, Q, K, V, Y, dY, dQ, dK, dV), _dense(cu_q, _I32, B + 1, dev, "cu_q"), _dense(cu_k, _I32, B + 1, dev, "cu_k"),
-          dq, dk, dv, _dense(ws, _U8, ws.numel(), dev, "ws"), ws.numel())
+          dq, dk, dv, _dense(ws, _U8, size, dev, "ws"), size)
     return dQ, dK, dV
 
 
@@ -233,9 +235,9 @@ def decode(shape: CacheShape, Q, cache, table, lens, scale=None, ws=None, Y=None
         Y = torch.empty(n, dtype=_BF16, device=Q.device)
     if ws is None:
         ws = alloc_decode_workspace(s, H, Q.device)
-    apart = []
+    apart, size = [], ws.numel()
     y = _rows(Y, n, dev, "Y", apart)
     _call(dev, "spt_attn_decode", _byref(s), H, dh ** -0.5 if scale is None else scale, _rows(Q, n, dev, "Q", apart), _strides(apart, Q, Y),
           *_pool(s, cache, dev), _dense(table, _I32, B * s.max_pages, dev, "table"), _dense(lens, _I32, B, dev, "lens"), y,
-          _dense(ws, _U8, ws.numel(), dev, "ws"), ws.numel())
+          _dense(ws, _U8, size, dev, "ws"), size)
     return Y
