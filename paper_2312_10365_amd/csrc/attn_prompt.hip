@@ -324,7 +324,7 @@ extern "C" int spt_attn_prompt_fwd(const spt_attn_shape_t* shape, const void* Q,
   ScopedKernelTimer timer(kSlotAttnFwd, st);
   const auto launch = [&](auto dh) {
     constexpr int DH = decltype(dh)::value;
-    const int owners = row_owners((int64_t)(s.Tq >> (7 - a.hshift)) * (s.H >> a.hshift), s.Tk, s.B);
+    const int owners = row_owners((int64_t)(s.Tq >> (7 - a.hshift)) * (s.H >> a.hshift), s.Tk, s);
     if (owners < 4) return owners == 2 ? launch_fwd<DH, 2, 4>(a, s, st) : launch_fwd<DH, 1, DH == 128 ? 4 : 8>(a, s, st);
     return two_groups(s, a.hshift) ? launch_fwd<DH, 4, 2>(a, s, st) : launch_fwd<DH, 4, 1>(a, s, st);
   };

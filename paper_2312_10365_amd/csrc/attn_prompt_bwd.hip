@@ -636,7 +636,7 @@ extern "C" int spt_attn_prompt_bwd(const spt_attn_shape_t* shape, const void* Q,
   a.c = s.scale * kLog2e;
   const int64_t q_tiles = (int64_t)(s.Tq >> (7 - a.hshift)) * (s.H >> a.hshift), kv_tiles = (int64_t)(s.Tk >> 7) * s.Hk;
   const bool few = (int64_t)s.Tq * a.G <= (int64_t)kFewRows * s.B || q_tiles <= kFewTiles;
-  const int q_owners = row_owners(q_tiles, s.Tk, s.B), kv_owners = row_owners(kv_tiles, (int64_t)s.Tq * a.G, s.B);
+  const int q_owners = row_owners(q_tiles, s.Tk, s), kv_owners = row_owners(kv_tiles, (int64_t)s.Tq * a.G, s);
   const hipStream_t st = static_cast<hipStream_t>(stream);
   const auto launches = [&](auto dh, auto exact) {
     constexpr int DH = decltype(dh)::value, ONES = DH == 128 ? 4 : 8;
