@@ -102,7 +102,7 @@ struct BwdSizes {
   static constexpr int OWN_BYTES = OWN ? OWNERS * TILE_BYTES : 0;
   static constexpr int SUMS = (GROUPS - 1) * OWNERS * DH * 128;                 // a gradient of the other groups
   static constexpr int Q_RING = kRing * 2 * TILE_BYTES;                         // of a group: tiles of K and V
-  static constexpr int Q_JOIN = SUMS + (GROUPS - 1) * OWNERS * 512, Q_RINGS = GROUPS * Q_RING + OWN_BYTES;
+  static constexpr int Q_JOIN = SUMS + (GROUPS - 1) * OWNERS * 768, Q_RINGS = GROUPS * Q_RING + OWN_BYTES;
   static constexpr int Q_SMEM = Q_RINGS > Q_JOIN ? Q_RINGS : Q_JOIN;
   static constexpr int KV_RING = kRing * (2 * TILE_BYTES + 256);                // tiles of Q and dY, their rows' offsets and -D
   static constexpr int KV_SMEM = GROUPS * KV_RING + OWN_BYTES;
@@ -200,7 +200,7 @@ __global__ __launch_bounds__((64 * OWNERS * GROUPS), 2) void prompt_bwd_q_kernel
   for (int d = 0; d < DT; ++d)
 #pragma unroll
     for (int r = 0; r < 16; ++r) o[d][r] = mean[d][r] = 0.f;
-  float left_over = 0.f, rounded = 0.f;                  // sum of dS: what D lacks; of dS as rounded
+  float left_over = 0.f, rounded = 0.f, mass = 0.f;      // sum of dS: what D lacks; of dS, of p (EXACT) as rounded
   NotFinite not_finite;
 
   auto first_products = [&](uint32_t kt, f32x16& s, f32x16& dp) {
@@ -236,8 +236,12 @@ __global__ __launch_bounds__((64 * OWNERS * GROUPS), 2) void prompt_bwd_q_kernel
       const uint32_t d = pack_bf16x2(d0, d1);
       w.p[r >> 3][(r & 7) >> 1] = pack_bf16x2(p0, p1);
       w.ds[r >> 3][(r & 7) >> 1] = d;
-      if constexpr (EXACT) w.rest[r >> 3][(r & 7) >> 1] = pack_bf16x2(d0 - lo_bf16(d), d1 - hi_bf16(d));
-      else rounded = sum2(d, rounded);
+      if constexpr (EXACT) {
+        w.rest[r >> 3][(r & 7) >> 1] = pack_bf16x2(d0 - lo_bf16(d), d1 - hi_bf16(d));
+        mass = sum2(w.p[r >> 3][(r & 7) >> 1], mass);
+      } else {
+        rounded = sum2(d, rounded);
+      }
     }
     return w;
   };
@@ -273,6 +277,7 @@ __global__ __launch_bounds__((64 * OWNERS * GROUPS), 2) void prompt_bwd_q_kernel
   }
   left_over += other_half(left_over);
   rounded = EXACT ? left_over : rounded + other_half(rounded);
+  if (EXACT) mass += other_half(mass);
   const int64_t stat = (int64_t)head * a.Tq;
   // rows that not all queries may see hold infinities or NaN: 0 times those is NaN
   if (full < ntile * kTile && __syncthreads_or(not_finite.found())) {
@@ -291,16 +296,19 @@ __global__ __launch_bounds__((64 * OWNERS * GROUPS), 2) void prompt_bwd_q_kernel
   if (GROUPS > 1) {
     add_groups<DH, OWNERS, GROUPS>(o, smem, wave, group, lane);
     add_groups<DH, OWNERS, GROUPS>(mean, smem, wave, group, lane);
-    float* rest = reinterpret_cast<float*>(smem + Sizes::SUMS) + wave * 128 + lane;
+    float* rest = reinterpret_cast<float*>(smem + Sizes::SUMS) + wave * 192 + lane;
     if (group > 0) {
-      rest[(group - 1) * OWNERS * 128] = left_over;
-      rest[(group - 1) * OWNERS * 128 + 64] = rounded;
+      float* mine = rest + (group - 1) * OWNERS * 192;
+      mine[0] = left_over;
+      mine[64] = rounded;
+      mine[128] = mass;
     }
     __syncthreads();
     if (group > 0) return;
     for (int g = 0; g < GROUPS - 1; ++g) {
-      left_over += rest[g * OWNERS * 128];
-      rounded += rest[g * OWNERS * 128 + 64];
+      left_over += rest[g * OWNERS * 192];
+      rounded += rest[g * OWNERS * 192 + 64];
+      mass += rest[g * OWNERS * 192 + 128];
     }
   }
   if (i0 + i >= nq) return;
@@ -308,12 +316,14 @@ __global__ __launch_bounds__((64 * OWNERS * GROUPS), 2) void prompt_bwd_q_kernel
     a.off[stat + row] = off;
     a.neg_d[stat + row] = -(D + left_over);
   }
+  // the p of `mean` were rounded: where one key has nearly all the weight, their sum is off by what that key's share is
+  const float off_by = EXACT && mass > 0.f ? rounded / mass : rounded;
   char* dq = a.dQ.p + row * a.dQ.row + (int64_t)head * a.dQ.head + h * 32;
 #pragma unroll
   for (int d = 0; d < DT; ++d) {
     float v[16];
 #pragma unroll
-    for (int r = 0; r < 16; ++r) v[r] = fmaf(-rounded, mean[d][r], o[d][r]) * a.scale;
+    for (int r = 0; r < 16; ++r) v[r] = fmaf(-off_by, mean[d][r], o[d][r]) * a.scale;
     *reinterpret_cast<bf16x8*>(dq + d * 64) = pack8(v);
     *reinterpret_cast<bf16x8*>(dq + d * 64 + 16) = pack8(v + 8);
   }
