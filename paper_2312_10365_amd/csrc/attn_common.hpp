@@ -64,23 +64,28 @@ inline int coarse_tiles(int64_t workgroups, int on_a_cu) {
   return rounds < 1 ? 0 : 63 - __builtin_clzll(rounds);
 }
 
-// Wavefronts of a workgroup that own 32 rows each: four, or, where there are so few workgroups (of four) that twice or four times as many fit
-// onto the chip at once, two or one; four or eight groups of them then share what passes through LDS, if that is enough (`through` rows of B
-// sequences).  us, four (in the forward with two groups) and fewer owners.  Forward: 8 heads of 128, 256 tokens 10.8 and 10.3, 512 14.3 and
-// 12.1; 2 heads of 64, 4000 42 and 23, 8 heads, 2000 (125 workgroups) 25.5 and 19.3.  Query side of the gradients: 12 heads of 64,
-// 160 11.5 and 12.2, 256 14.1 and 12.6, 512 20.7 and 14.0, 1024 28 and 17; 2 heads, 4000 106 and 32.  Key side: 12 heads of 64, 77 10.5
-// and 11.8, 160 13.4 and 12.1, 512 24.5 and 14.3, 1024 33 and 18.5; 32 heads of 64 on 8, 512 61 and 23, of 128 on 8 63 and 37, two of
-// 1000 117 and 77.  One owner and two: 24 heads of 64, 384 (72 workgroups) query side 20.6 and 12.9, key side 20.3 and 13.0.
-// Up to twice as many still go in two rounds of two owners, where there is much to share and the second round fills up: with `causal`, whose
-// workgroups are unequal, and 64-wide heads, of which one of four owners leaves a CU's wavefronts waiting.  us, four owners and two, `causal`: 8
-// heads, 4000 tokens (250 workgroups), of 64 forward 44 and 34, query side 89 and 49, key side 105 and 55, of 128 58 and 54, 132 and 81, 114 and
-// 87; 31 sequences of 4 to 1993, 4 heads of 64 on 2 key side 109 and 49; 4 of 512, 16 heads of 64 query side 19.2 and 21.6; two of 4000, 8 heads of
-// 128 (500) key side 137 and 169.  All keys seen: 8 heads of 64, 4000 48 and 50, 90 and 81, 105 and 91, of 128 69 and 88, 142 and 137, 129 and 150.
-constexpr int kFewTiles = 64;
-inline int row_owners(int64_t workgroups, int64_t through, const spt_attn_shape_t& s) {
-  if (workgroups > 4 * kFewTiles || through < 192 * (int64_t)s.B) return 4;
-  if (workgroups <= 2 * kFewTiles) return workgroups <= kFewTiles ? 1 : 2;
-  return through >= 640 * (int64_t)s.B && (s.causal || s.dh == 64) ? 2 : 4;
+// Workgroups of 1 << shift rows for each of `heads`: about as many as there are, and one for each sequence at least.
+inline int64_t row_workgroups(int T, int shift, int B, int heads) { return (int64_t)(T >> shift > B ? T >> shift : B) * heads; }
+
+// Wavefronts of a workgroup that own 32 rows each (of up to 1 << hshift heads): four, or, where all workgroups still fit onto the chip at once,
+// two or one; four or eight groups of them then share what passes through LDS, if that is enough (`through` rows of B sequences).
+// us, four (in the forward with two groups) and fewer owners.  Forward: 8 heads of 128, 256 tokens 10.8 and 10.3, 512 14.3 and 12.1; 2 heads of
+// 64, 4000 42 and 23, 8 heads, 2000 25.5 and 19.3.  Query side of the gradients: 12 heads of 64, 160 11.5 and 12.2, 256 14.1 and 12.6, 512 20.7
+// and 14.0, 1024 28 and 17; 2 heads, 4000 106 and 32; 12 heads, 16 times 8 queries behind 500 keys 19.4 and 13.3.  Key side: 12 heads of 64, 77
+// 10.5 and 11.8, 160 13.4 and 12.1, 512 24.5 and 14.3, 1024 33 and 18.5; 32 heads of 64 on 8, 512 61 and 23, of 128 on 8 63 and 37, two of
+// 1000 117 and 77.  One owner and two: 24 heads of 64, 384 (288 workgroups of one) query side 20.6 and 12.9, key side 20.3 and 13.0.  One owner
+// and four: 21 times 3 queries behind 1000 keys, 64 heads of 64 on 16 (1344 of one) forward 67 and 27.
+// Two rounds of two owners still gain where there is much to share and the second round fills up: with `causal`, whose workgroups are unequal,
+// and 64-wide heads, of which one workgroup of four leaves a CU's wavefronts waiting.  us, four owners and two, `causal`: 8 heads, 4000 tokens (500
+// workgroups), of 64 forward 44 and 34, query side 89 and 49, key side 105 and 55, of 128 58 and 54, 132 and 81, 114 and 87; 31 sequences of 4 to
+// 1993, 4 heads of 64 on 2 key side 109 and 49; 4 of 512, 16 heads of 64 query side 19.2 and 21.6; two of 4000, 8 heads of 128 (1000) key side
+// 137 and 169.  All keys seen: 8 heads of 64, 4000 48 and 50, 90 and 81, 105 and 91, of 128 69 and 88, 142 and 137, 129 and 150.
+inline int row_owners(int T, int heads, int hshift, int64_t through, const spt_attn_shape_t& s) {
+  const int hs = hshift < 1 ? hshift : 1;
+  const int64_t ones = row_workgroups(T, 5, s.B, heads), twos = row_workgroups(T, 6 - hs, s.B, heads >> hs), B = s.B;
+  if (through < 192 * B) return 4;
+  if (ones <= 256) return 1;
+  return twos <= 256 || (twos <= 512 && through >= 640 * B && (s.causal || s.dh == 64)) ? 2 : 4;
 }
 
 // ---- device side

@@ -265,7 +265,7 @@ __global__ __launch_bounds__((64 * OWNERS * GROUPS), 2) void prompt_fwd_kernel(c
 // resident) 154 and 158; four of 512, which have few tiles to share, 23.0 and 26.2; 12 heads of 64, one of 8000 146 and 133; 32 heads of 64,
 // four of 1024 (four workgroups on a CU) 33 and 37.
 bool two_groups(const spt_attn_shape_t& s, int hshift) {
-  const int64_t workgroups = (int64_t)(s.Tq >> (7 - hshift)) * (s.H >> hshift), resident = 256 * (s.dh == 128 ? 2 : 3);
+  const int64_t workgroups = row_workgroups(s.Tq, 7 - hshift, s.B, s.H >> hshift), resident = 256 * (s.dh == 128 ? 2 : 3);
   return workgroups <= resident / 2 || (workgroups <= resident && s.Tk >= 1024 * (int64_t)s.B);
 }
 
@@ -324,7 +324,7 @@ extern "C" int spt_attn_prompt_fwd(const spt_attn_shape_t* shape, const void* Q,
   ScopedKernelTimer timer(kSlotAttnFwd, st);
   const auto launch = [&](auto dh) {
     constexpr int DH = decltype(dh)::value;
-    const int owners = row_owners((int64_t)(s.Tq >> (7 - a.hshift)) * (s.H >> a.hshift), s.Tk, s);
+    const int owners = row_owners(s.Tq, s.H, a.hshift, s.Tk, s);
     if (owners < 4) return owners == 2 ? launch_fwd<DH, 2, 4>(a, s, st) : launch_fwd<DH, 1, DH == 128 ? 4 : 8>(a, s, st);
     return two_groups(s, a.hshift) ? launch_fwd<DH, 4, 2>(a, s, st) : launch_fwd<DH, 4, 1>(a, s, st);
   };

@@ -50,6 +50,7 @@ struct Weights<true> { u32x4 p[2], ds[2], rest[2]; };
 // up to 80, 1.45 for longer ones, 1.0 exact.  Key side, us, rounded and exact: 8192 tokens, 32 heads of 128 on 8: sequences of 32 95 and 99,
 // of 64 71 and 75, of 128 61 and 65; 32 heads of 64: 57 and 58, 44 and 47, 46 and 48, of 512 67 and 76.
 constexpr int kFewRows = 128;     // of queries of a sequence and key head, on average
+constexpr int kFewTiles = 256;    // of 32 queries and a head, in all
 
 // p and dS of one pair, from its rows in memory.
 struct PairGrad { float p, ds; };
@@ -644,9 +645,8 @@ extern "C" int spt_attn_prompt_bwd(const spt_attn_shape_t* shape, const void* Q,
   a.causal = s.causal;
   a.scale = s.scale;
   a.c = s.scale * kLog2e;
-  const int64_t q_tiles = (int64_t)(s.Tq >> (7 - a.hshift)) * (s.H >> a.hshift), kv_tiles = (int64_t)(s.Tk >> 7) * s.Hk;
-  const bool few = (int64_t)s.Tq * a.G <= (int64_t)kFewRows * s.B || q_tiles <= kFewTiles;
-  const int q_owners = row_owners(q_tiles, s.Tk, s), kv_owners = row_owners(kv_tiles, (int64_t)s.Tq * a.G, s);
+  const bool few = (int64_t)s.Tq * a.G <= (int64_t)kFewRows * s.B || (int64_t)(s.Tq >> 5) * s.H <= kFewTiles;
+  const int q_owners = row_owners(s.Tq, s.H, a.hshift, s.Tk, s), kv_owners = row_owners(s.Tk, s.Hk, 0, (int64_t)s.Tq * a.G, s);
   const hipStream_t st = static_cast<hipStream_t>(stream);
   const auto launches = [&](auto dh, auto exact) {
     constexpr int DH = decltype(dh)::value, ONES = DH == 128 ? 4 : 8;

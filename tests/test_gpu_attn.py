@@ -94,6 +94,8 @@ FEW = {   # few workgroups with much to read: rows in 32s, or on one side only
     "rows_in_64s_full": ([300, 1, 451], [290, 0, 461], 16, 16, False),
     "rows_in_64s_groups_of_4": ([300, 0, 451], [300, 0, 451], 16, 4, True),
     "rows_in_64s_groups_of_2": ([300, 33, 420], [300, 33, 420], 16, 8, True),
+    "a_few_tokens_each": ([3, 1, 2] * 5, [203, 301, 150] * 5, 64, 16, True),
+    "eight_tokens_each": ([8] * 16, [208] * 16, 12, 12, True),
     "two_rounds_of_64s": ([1500, 3], [1500, 3], 16, 16, True),
     "two_rounds_of_64s_full": ([30, 1400], [70, 1400], 20, 10, False),
     "keys_in_64s": ([300, 33, 420], [300, 33, 420], 32, 16, True),
