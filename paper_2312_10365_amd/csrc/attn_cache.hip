@@ -176,7 +176,7 @@ struct DecodeArgs {
   float cs;                       // scale log2 e
 };
 
-__device__ __forceinline__ int units_of(int len) { return (len + kUnit - 1) / kUnit; }
+__device__ __forceinline__ int units_of(int len) { return len / kUnit + (len % kUnit != 0); }   // (len + 31 may pass 31 bits)
 __device__ __forceinline__ int seq_len(const DecodeArgs& a, int len) { return min(max(len, 0), a.c.max_pages << a.c.page_shift); }
 __device__ __forceinline__ int seq_units(const DecodeArgs& a, int b) { return units_of(seq_len(a, a.lens[b])); }
 

@@ -1,0 +1,33 @@
+"""Full attention, the cache and single tokens at the ends of what their arguments allow, against the definition in 64 bits
+(attn_ref.py)."""
+import numpy as np
+import pytest
+import torch
+
+import attn_ref as ref
+from paper_2312_10365_amd import attn
+
+pytestmark = pytest.mark.gpu
+
+
+def ints(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def test_decode_lengths_up_to_the_widest_table():
+    """A table of 2^31 - 16 tokens, of which four pages are there (the others are left out): lengths at whose end the count of
+    units of 32 tokens would pass 31 bits, and lengths in front of it."""
+    page, width, dh = 16, (1 << 27) - 1, 64
+    shape = attn.make_cache_shape(4, page, 1, dh, 1, width)
+    table = torch.full((1, width), -1, dtype=torch.int32, device="cuda")
+    at = [0, 1, 70_000_000, width - 1]                            # the pages that are there
+    table[0, torch.tensor(at, device="cuda")] = ints([2, 0, 3, 1])
+    cache = attn.alloc_cache(shape)
+    K, V, Q = ref.bf16(64, 1, dh, seed=1), ref.bf16(64, 1, dh, seed=2), ref.bf16(1, 1, dh, seed=3)
+    for n, (p, slot) in enumerate(zip(at, (2, 0, 3, 1))):
+        cache.K[slot, 0], cache.V[slot, 0] = K[16 * n:16 * n + 16, 0].cuda(), V[16 * n:16 * n + 16, 0].cuda()
+    q, k, v = (ref.f64(t) for t in (Q, K, V))
+    for length in (width * page, width * page - 1, width * page - 15, width * page - 16, width * page - 17, 70_000_000 * page + 3, 9):
+        there = np.concatenate([16 * n + np.arange(16)[p * page + np.arange(16) < length] for n, p in enumerate(at)])
+        want = ref.prompt(q, k[there], v[there], [1], [len(there)], False, dh ** -0.5)["Y"]
+        ref.check(f"Y, {length} tokens", attn.decode(shape, Q.cuda(), cache, table, ints([length])), *want)
