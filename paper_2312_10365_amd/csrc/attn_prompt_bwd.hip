@@ -75,22 +75,35 @@ __device__ __forceinline__ void fetch_pair(int tid, const char* x, int64_t xrow,
   }
 }
 
+// A row of dQ the plain way, over the n keys that it sees: lanes take keys for the pairs, dims for the sums.  Returns what D lacks,
+// the sum of the row's dS, and takes it off as the other rows do: times the mean of the keys.
 template <int DH>
-__device__ __forceinline__ void slow_dq_row(const BwdArgs& a, const char* q, const char* dy, const char* k, const char* v, int n, float off,
-                                            float D, char* dq) {
+__device__ __forceinline__ float slow_dq_row(const BwdArgs& a, const char* q, const char* dy, const char* k, const char* v, int n, float off,
+                                             float D, char* dq) {
   const int lane = threadIdx.x & 63;
-  float acc[DH / 64] = {};
+  float acc[DH / 64] = {}, mean[DH / 64] = {}, left_over = 0.f, mass = 0.f;
   for (int j0 = 0; j0 < n; j0 += 64) {
     const int j = j0 + lane;
-    const float ds = j < n ? pair_grad(q, k + j * a.K.row, dy, v + j * a.V.row, DH, a.c, off, D).ds : 0.f;
+    PairGrad x = {0.f, 0.f};
+    if (j < n) x = pair_grad(q, k + j * a.K.row, dy, v + j * a.V.row, DH, a.c, off, D);
+    left_over += x.ds;
+    mass += x.p;
     for (int e = 0; e < min(64, n - j0); ++e) {
-      const float w = __shfl(ds, e);
+      const float p = __shfl(x.p, e), ds = __shfl(x.ds, e);
 #pragma unroll
-      for (int d = 0; d < DH / 64; ++d) acc[d] = fmaf(w, bf16_at(k + (j0 + e) * a.K.row + (lane + 64 * d) * 2), acc[d]);
+      for (int d = 0; d < DH / 64; ++d) {
+        const float kd = bf16_at(k + (j0 + e) * a.K.row + (lane + 64 * d) * 2);
+        acc[d] = fmaf(ds, kd, acc[d]);
+        mean[d] = fmaf(p, kd, mean[d]);
+      }
     }
   }
+  left_over = wave_sum(left_over);
+  mass = wave_sum(mass);
+  const float off_by = mass > 0.f ? left_over / mass : 0.f;
 #pragma unroll
-  for (int d = 0; d < DH / 64; ++d) reinterpret_cast<uint16_t*>(dq)[lane + 64 * d] = (uint16_t)pack_bf16x2(acc[d] * a.scale, 0.f);
+  for (int d = 0; d < DH / 64; ++d) reinterpret_cast<uint16_t*>(dq)[lane + 64 * d] = (uint16_t)pack_bf16x2(fmaf(-off_by, mean[d], acc[d]) * a.scale, 0.f);
+  return left_over;
 }
 
 // Sizes of a workgroup of GROUPS groups of OWNERS wavefronts.  A wavefront of a group owns 32 rows, the groups go through every GROUPS-th
@@ -285,12 +298,12 @@ __global__ __launch_bounds__((64 * OWNERS * GROUPS), 2) void prompt_bwd_q_kernel
     for (int r = group; r < min(32, nq - i0); r += GROUPS) {
       const int64_t at = sq.first + i0 + r;
       const float Dr = __shfl(D, r), offr = __shfl(off, r);
+      const float left = slow_dq_row<DH>(a, a.Q.p + at * a.Q.row + (int64_t)head * a.Q.head, a.dY.p + at * a.dY.row + (int64_t)head * a.dY.head, kbase, vbase,
+                                         a.causal ? min(nk, i0 + r + ahead + 1) : nk, offr, Dr, a.dQ.p + at * a.dQ.row + (int64_t)head * a.dQ.head);
       if (lane == 0) {
         a.off[stat + at] = offr;
-        a.neg_d[stat + at] = -Dr;
+        a.neg_d[stat + at] = -(Dr + left);
       }
-      slow_dq_row<DH>(a, a.Q.p + at * a.Q.row + (int64_t)head * a.Q.head, a.dY.p + at * a.dY.row + (int64_t)head * a.dY.head, kbase, vbase,
-                      a.causal ? min(nk, i0 + r + ahead + 1) : nk, offr, Dr, a.dQ.p + at * a.dQ.row + (int64_t)head * a.dQ.head);
     }
     return;
   }

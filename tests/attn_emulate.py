@@ -1,17 +1,17 @@
-"""The kernels' own arithmetic in 64 bits with their roundings to bf16 at the places where they make them, one sequence at a
-time: how far off a result is to be as a whole (2-norm), where the bounds of attn_ref.py, which add up the worst of every
-element, would not tell one rounding from two.
+"""The kernels' own arithmetic in 64 bits with their roundings to bf16 at the places where they make them: how far off a
+result is to be as a whole (2-norm), where the bounds of attn_ref.py, which add up the worst of every element, would not
+tell one rounding from two.
 
-A rounding's error is even over half a step, so errors of other inputs, another order of sums or other maxima to which weights are scaled have
-the same second moment; the norm over n values fluctuates by about 1 / sqrt(n) of it.  FACTOR leaves 25 % for that and for
-the operations of 32 bits (2^-24 each, against 2^-9).  `mistake` leaves out or turns round what the kernels do about their roundings: a test of
-the limits, which must not hold then."""
+A rounding's error is even over half a step, so errors of another order of sums, or of weights scaled to another maximum,
+have the same second moment; the norm over n values fluctuates by about 1 / sqrt(n) of itself, here a few percent.  FACTOR leaves 20 % for that and
+for the operations of 32 bits (2^-24 each, against 2^-9).  `mistake` leaves out or turns round what the kernels do about
+their roundings: the limits must not hold then."""
 import numpy as np
 import torch
 
 import attn_ref as ref
 
-FACTOR = 1.25
+FACTOR = 1.2
 
 
 def bf(x):
@@ -23,18 +23,19 @@ def two(x):
     return hi + bf(x - hi)
 
 
-def forward(q, k, v, scale, seen, mistake=None):
-    """Y of one head: weights, scaled to their row's largest, go into their product as one bf16."""
+def forward(q, k, v, scale, seen):
+    """Y of one head: weights go into their product as one bf16, scaled to a maximum that may be one of the row's earlier
+    ones: to any number, here another for every row, evenly over a power of two."""
     s = np.where(seen, scale * (q @ k.T), -np.inf)
     top = s.max(-1, initial=-np.inf, keepdims=True)
-    w = np.where(seen, np.exp(s - np.where(top == -np.inf, 0.0, top)), 0.0)
+    w = np.where(seen, np.exp(s - np.where(top == -np.inf, 0.0, top)), 0.0) * 2.0 ** (np.arange(len(q)) * 0.618034 % 1.0)[:, None]
     total = w.sum(-1, keepdims=True)
     return bf(bf(w) @ v / np.where(total == 0, 1.0, total))
 
 
-def backward(q, k, v, dy, scale, seen, exact_ds, mistake=None):
-    """dQ, and dK, dV before their rounding, of one head.  Y is rounded, so D is off: the sum of a row's dS, which is 0 but for
-    that, is taken off.  dS is the sum of two bf16 (`exact_ds`) or one."""
+def backward(q, k, v, dy, scale, seen, exact_ds, mistake):
+    """dQ, and dK, dV before their rounding, of one head.  Y is rounded, so D is off: the sum of a row's dS, which is 0 but
+    for that, is taken off.  dS is the sum of two bf16 (`exact_ds`) or one."""
     p, _ = ref.softmax(scale * (q @ k.T), seen)
     D = (dy * forward(q, k, v, scale, seen)).sum(-1, keepdims=True)
     dP = dy @ v.T
@@ -48,29 +49,52 @@ def backward(q, k, v, dy, scale, seen, exact_ds, mistake=None):
     return dQ, scale * rounded(p * (dP - (D + sign * left))).T @ q, p_in.T @ dy
 
 
-def prompt(Q, K, V, lens_q, lens_k, causal, scale, dY, exact_ds, mistake=None):
-    """All sequences and heads, packed: {name: value}."""
+def _heads(f, Q, K, V, lens_q, lens_k, causal, dY, gone):
+    """f's {name: values} of all sequences and heads, packed.  `gone`: rows of K whose scores are -inf."""
     G = Q.shape[1] // K.shape[1]
     out = {"Y": np.zeros(Q.shape), "dQ": np.zeros(Q.shape), "dK": np.zeros(K.shape), "dV": np.zeros(K.shape)}
+    there = ~np.isin(np.arange(len(K)), gone)
+    K = np.where(there[:, None, None], K, 0.0)
     a = b = 0
     for nq, nk in zip(lens_q, lens_k):
-        rq, rk, seen = slice(a, a + nq), slice(b, b + nk), ref.visible(nq, nk, causal)
+        rq, rk = slice(a, a + nq), slice(b, b + nk)
+        seen = ref.visible(nq, nk, causal) & there[None, rk]
         for h in range(Q.shape[1]):
-            one = Q[rq, h], K[rk, h // G], V[rk, h // G]
-            out["Y"][rq, h] = forward(*one, scale, seen)
-            dQ, dK, dV = backward(*one, dY[rq, h], scale, seen, exact_ds, mistake)
-            out["dQ"][rq, h] = dQ
-            out["dK"][rk, h // G] += dK
-            out["dV"][rk, h // G] += dV
+            one = f(Q[rq, h], K[rk, h // G], V[rk, h // G], dY[rq, h], seen)
+            for n, x in one.items():
+                if n in ("dK", "dV"):
+                    out[n][rk, h // G] += x
+                else:
+                    out[n][rq, h] = x
         a, b = a + nq, b + nk
+    return out
+
+
+def prompt(Q, K, V, lens_q, lens_k, causal, scale, dY, exact_ds, mistake=None, gone=()):
+    """{name: value} of a backward pass and its forward, with the kernels' roundings."""
+    def f(q, k, v, dy, seen):
+        return {"Y": forward(q, k, v, scale, seen)} | dict(zip(("dQ", "dK", "dV"), backward(q, k, v, dy, scale, seen, exact_ds, mistake)))
+    out = _heads(f, Q, K, V, lens_q, lens_k, causal, dY, gone)
     return out | {n: bf(out[n]) for n in ("dK", "dV")}
 
 
-def decode(q, k, v, scale, mistake=None):
-    """One query head over its keys: weights go into their product as the sum of two bf16."""
-    s = scale * (k @ q)
-    w = np.exp(s - s.max())
-    return bf(((bf if mistake == "one weight" else two)(w) @ v) / w.sum())
+def exact(Q, K, V, lens_q, lens_k, causal, scale, dY, gone=()):
+    """The same without roundings."""
+    def f(q, k, v, dy, seen):
+        return {n: x for n, (x, _) in ref.head(q, k, v, scale, seen, dy).items() if n != "lse"}
+    return _heads(f, Q, K, V, lens_q, lens_k, causal, dY, gone)
+
+
+def decode(Q, K, V, lens, scale, mistake=None, exact=False):
+    """Y [B, H, dh] of single tokens: weights go into their product as the sum of two bf16."""
+    G, ends, Y = Q.shape[1] // K.shape[1], np.cumsum([0] + list(lens)), np.zeros(Q.shape)
+    for b in range(len(lens)):
+        rows = slice(ends[b], ends[b + 1])
+        for h in range(Q.shape[1]):
+            s = scale * (K[rows, h // G] @ Q[b, h])
+            w = np.exp(s - s.max())
+            Y[b, h] = (w if exact else bf(w) if mistake == "one weight" else two(w)) @ V[rows, h // G] / w.sum()
+    return Y if exact else bf(Y)
 
 
 def off(got, want):
