@@ -13,6 +13,35 @@ import attn_ref as ref
 
 FACTOR = 1.2
 
+# Passes that reach every form of the gradients' kernels: lengths of queries, of keys, H, Hk, head dimensions, causal, whether dS is the sum
+# of two bf16, rows of Q and of K behind the last sequence (forms are chosen by the rows of the tensors); behind each the
+# wavefronts of a workgroup that own 32 rows, on the side of the queries and of the keys
+PASSES = {
+    "short": ([2 + i % 8 for i in range(40)], None, 4, 2, (64, 128), True, True, 0, 0),                   # 4, 4
+    "short_full": ([9 - i % 8 for i in range(40)], None, 3, 3, (64, 128), False, True, 0, 0),             # 4, 4
+    "few": ([170, 330], None, 4, 2, (64, 128), True, True, 0, 0),                                         # 1, 1
+    "few_full": ([330, 170], None, 2, 2, (64, 128), False, True, 0, 0),                                   # 1, 1
+    "parts": ([100] * 12, [300] * 12, 8, 8, (64, 128), True, True, 0, 0),                                 # 2, 4
+    "more_keys": ([200], [1200], 8, 8, (64, 128), False, True, 0, 0),                                     # 1, 2
+    "rows_in_64s": ([300, 250], None, 16, 16, (64, 128), True, False, 0, 0),                              # 2, 2
+    "grouped": ([130] * 4, None, 32, 8, (64, 128), True, False, 0, 0),                                    # 4, 1
+    "rows_in_128s": ([150] * 8, None, 8, 8, (64, 128), True, False, 0, 0),                                # 4, 4
+    "rows_in_128s_full": ([150] * 8, None, 8, 8, (64, 128), False, False, 0, 0),                          # 4, 4
+    "keys_in_256s": ([300, 270], None, 4, 4, (128,), False, False, 9000, 16000),                          # 4, 8
+    "keys_in_256s_exact": ([300, 270], None, 4, 4, (128,), False, True, 0, 16000),                        # 1, 8
+}
+# single tokens: lengths, H, Hk, dh, tokens of a page
+TOKENS = {
+    "four_heads": ([300, 100, 2000], 8, 2, 128, 16),
+    "twenty_heads": ([500, 1300], 40, 2, 64, 64),
+    "own_keys": ([900, 333], 6, 6, 64, 256),
+}
+
+
+def inputs(lens_q, lens_k, H, Hk, dh, sharp, seed=1):
+    Q, K, V, dY = (ref.bf16(sum(n), h, dh, seed=seed + i) for i, (n, h) in enumerate(((lens_q, H), (lens_k, Hk), (lens_k, Hk), (lens_q, H))))
+    return (Q.float() * sharp).to(torch.bfloat16), K, V, dY
+
 
 def bf(x):
     return torch.from_numpy(np.ascontiguousarray(x)).to(torch.bfloat16).double().numpy()

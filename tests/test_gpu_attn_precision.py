@@ -1,4 +1,4 @@
-"""Errors of full attention's gradients as a whole (2-norm) against the definition in 64 bits, within what their roundings make
+"""Errors of full attention, of its gradients and of single tokens as a whole (2-norm) against the definition in 64 bits, within what their roundings make
 (attn_emulate.py)."""
 import numpy as np
 import pytest
@@ -11,17 +11,53 @@ from paper_2312_10365_amd import attn
 pytestmark = pytest.mark.gpu
 
 
-def inputs(lens_q, lens_k, H, Hk, dh, sharp, seed=1):
-    Q, K, V, dY = (ref.bf16(sum(n), h, dh, seed=seed + i) for i, (n, h) in enumerate(((lens_q, H), (lens_k, Hk), (lens_k, Hk), (lens_q, H))))
-    return (Q.float() * sharp).to(torch.bfloat16), K, V, dY
-
-
-def run(lens_q, lens_k, causal, Q, K, V, dY):
+def run(lens_q, lens_k, causal, Q, K, V, dY, spare_q=0, spare_k=0):
+    nq, nk = Q.shape[0], K.shape[0]
+    Q, K, V, dY = (torch.cat([t, t.new_zeros(n, *t.shape[1:])]) for t, n in ((Q, spare_q), (K, spare_k), (V, spare_k), (dY, spare_q)))
     shape = attn.make_shape(len(lens_q), Q.shape[0], K.shape[0], Q.shape[1], K.shape[1], Q.shape[2], causal)
     cu_q, cu_k = ref.sums(lens_q).cuda(), ref.sums(lens_k).cuda()
     Q, K, V, dY = (t.cuda() for t in (Q, K, V, dY))
     Y, lse = attn.prompt_fwd(shape, Q, K, V, cu_q, cu_k)
-    return dict(zip(("Y", "dQ", "dK", "dV"), map(ref.f64, (Y, *attn.prompt_bwd(shape, Q, K, V, Y, dY, lse, cu_q, cu_k)))))
+    dQ, dK, dV = attn.prompt_bwd(shape, Q, K, V, Y, dY, lse, cu_q, cu_k)
+    return {"Y": ref.f64(Y)[:nq], "dQ": ref.f64(dQ)[:nq], "dK": ref.f64(dK)[:nk], "dV": ref.f64(dV)[:nk]}
+
+
+@pytest.mark.parametrize("sharp", [1.0, 12.0])
+@pytest.mark.parametrize("name,dh", [(n, dh) for n, p in emulate.PASSES.items() for dh in p[4]])
+def test_gradients(name, dh, sharp):
+    lens_q, lens_k, H, Hk, _, causal, exact_ds, *spare = emulate.PASSES[name]
+    lens_k = lens_k or lens_q
+    Q, K, V, dY = emulate.inputs(lens_q, lens_k, H, Hk, dh, sharp)
+    got = run(lens_q, lens_k, causal, Q, K, V, dY, *spare)
+    args = *map(ref.f64, (Q, K, V)), lens_q, lens_k, causal, dh ** -0.5, ref.f64(dY)
+    want, rounded = emulate.exact(*args), emulate.prompt(*args, exact_ds)
+    off = {x: (emulate.off(got[x], want[x]), emulate.off(rounded[x], want[x])) for x in got}
+    print({x: f"{a:.2e} of {b:.2e}" for x, (a, b) in off.items()})
+    assert all(a <= emulate.FACTOR * b for a, b in off.values()), off
+
+
+@pytest.mark.parametrize("fmt", [attn.CACHE_BF16, attn.CACHE_E4M3])
+@pytest.mark.parametrize("wide", [False, True])
+@pytest.mark.parametrize("sharp", [1.0, 4.0])
+@pytest.mark.parametrize("name", emulate.TOKENS)
+def test_single_tokens(name, sharp, wide, fmt):
+    lens, H, Hk, dh, page = emulate.TOKENS[name]
+    Q, K, V, _ = emulate.inputs([1] * len(lens), lens, H, Hk, dh, sharp)
+    need = [-(-n // page) for n in lens]
+    width = -(-4096 // page) if wide else max(need)
+    table = torch.full((len(lens), width), -1, dtype=torch.int32)
+    for b, n in enumerate(need):
+        table[b, :n] = torch.arange(n) + sum(need[:b])
+    shape, table = attn.make_cache_shape(sum(need), page, Hk, dh, len(lens), width, fmt), table.cuda()
+    cache, start, cu = attn.alloc_cache(shape), torch.zeros(len(lens), dtype=torch.int32, device="cuda"), ref.sums(lens).cuda()
+    attn.cache_write(shape, K.cuda(), V.cuda(), cache, table, start, cu)
+    k, v = (ref.f64(t) if fmt == attn.CACHE_BF16 else ref.values(*ref.quantise(ref.f64(t))) for t in (K, V))
+    got = ref.f64(attn.decode(shape, Q.cuda(), cache, table, torch.tensor(lens, dtype=torch.int32, device="cuda")))
+    args = ref.f64(Q), k, v, lens, dh ** -0.5
+    want = emulate.decode(*args, exact=True)
+    off = emulate.off(got, want), emulate.off(emulate.decode(*args), want)
+    print("{:.2e} of {:.2e}".format(*off))
+    assert off[0] <= emulate.FACTOR * off[1], off
 
 
 @pytest.mark.parametrize("dh", [64, 128])
@@ -31,7 +67,7 @@ def test_rows_whose_hidden_keys_are_not_finite(dh, H, Hk, lens, exact_ds):
     """A key of -inf, with scores of -inf for all that see it: rows in front of it that share a workgroup with rows that do lose
     nothing, nor do the gradients of the keys that any of them see."""
     at = 70
-    Q, K, V, dY = inputs(lens, lens, H, Hk, dh, 12.0, seed=21)
+    Q, K, V, dY = emulate.inputs(lens, lens, H, Hk, dh, 12.0, seed=21)
     Q[:, :, 3] = Q[:, :, 3].abs() + 1.0
     K[at, :, 3] = float("-inf")
     got = run(lens, lens, True, Q, K, V, dY)
