@@ -267,8 +267,9 @@ struct DecodeState {
     float x[8], top = -INFINITY;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      float v = s[e >> 2][e & 3] * cs;
-      if (E4M3) v = __builtin_ldexpf(v, (int)((kb[e >> 2] >> (8 * (e & 3))) & 255u) - 127);
+      float v = s[e >> 2][e & 3];
+      if (E4M3) v = __builtin_ldexpf(v, (int)((kb[e >> 2] >> (8 * (e & 3))) & 255u) - 127);   // (first: codes times a large scale may pass what fp32 holds)
+      v *= cs;
       x[e] = (there >> (16 * (e >> 2) + 4 * c + (e & 3))) & 1 ? v : -INFINITY;
       top = fmaxf(top, x[e]);
     }

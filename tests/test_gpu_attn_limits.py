@@ -31,3 +31,20 @@ def test_decode_lengths_up_to_the_widest_table():
         there = np.concatenate([16 * n + np.arange(16)[p * page + np.arange(16) < length] for n, p in enumerate(at)])
         want = ref.prompt(q, k[there], v[there], [1], [len(there)], False, dh ** -0.5)["Y"]
         ref.check(f"Y, {length} tokens", attn.decode(shape, Q.cuda(), cache, table, ints([length])), *want)
+
+
+@pytest.mark.parametrize("fmt", [attn.CACHE_BF16, attn.CACHE_E4M3])
+@pytest.mark.parametrize("width", [7, 200])
+@pytest.mark.parametrize("std,scale", [(2.0 ** -100, 2.0 ** 97), (2.0 ** -112, 2.0 ** 109), (2.0 ** -123, 2.0 ** 120), (2.0 ** 100, 2.0 ** -103)])
+def test_decode_small_keys_and_large_scales(fmt, width, std, scale):
+    """Scores of the usual size from keys and a scale at both ends of what fp32 holds."""
+    lens, page, Hk, dh = [100, 37], 16, 2, 64
+    K, V, Q = ref.bf16(sum(lens), Hk, dh, seed=1, std=std), ref.bf16(sum(lens), Hk, dh, seed=2), ref.bf16(2, 4, dh, seed=3)
+    table = torch.full((2, width), -1, dtype=torch.int32)
+    table[0, :7], table[1, :3] = torch.arange(7), torch.arange(7, 10)
+    shape, table = attn.make_cache_shape(10, page, Hk, dh, 2, width, fmt), table.cuda()
+    cache = attn.alloc_cache(shape)
+    attn.cache_write(shape, K.cuda(), V.cuda(), cache, table, ints([0, 0]), ref.sums(lens).cuda())
+    k, v = (ref.f64(t) if fmt == attn.CACHE_BF16 else ref.values(*ref.quantise(ref.f64(t))) for t in (K, V))
+    want = ref.prompt(ref.f64(Q), k, v, [1, 1], lens, False, scale)["Y"]
+    ref.check("Y", attn.decode(shape, Q.cuda(), cache, table, ints(lens), scale=scale), *want)
