@@ -323,6 +323,7 @@ struct NotFinite {
 #pragma unroll
     for (int e = 0; e < 4; ++e) top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, x[e] & 0x7FFF7FFFu));
   }
+  __device__ __forceinline__ void mark(bool yes) { top[0] = yes ? 0x7F80 : top[0]; }
   __device__ __forceinline__ bool found() const { return top[0] >= 0x7F80 || top[1] >= 0x7F80; }
 };
 

@@ -18,6 +18,9 @@ using namespace spt;
 namespace {
 
 constexpr float kLazy = 8.f;   // a row's maximum may be this much (log2) above what its sums are scaled by
+// From this maximum (log2) on rows are taken the plain way.  c s - m is formed without a rounding between, m was rounded: by up to 8 here, so
+// that weights stay below 2^16; a maximum of 2^32 would be off by 256, and all weights of the row 0 or infinite.
+constexpr float kFar = 0x1p28f;
 
 struct FwdArgs {
   AttnRows Q, K, V, Y;
@@ -28,7 +31,7 @@ struct FwdArgs {
   float c;
 };
 
-// A row the plain way, for wavefronts that met infinities or NaN in rows that some of their queries must not see: lanes
+// A row the plain way, for wavefronts that met infinities or NaN in rows that some of their queries must not see, or scores too far from 0: lanes
 // take keys for the scores, dims for the sum, and only the `n` visible keys are touched.
 template <int DH>
 __device__ __forceinline__ void slow_row(const char* q, const char* k, int64_t kstep, const char* v, int64_t vstep, int n, float c, char* y,
@@ -122,7 +125,7 @@ __global__ __launch_bounds__((64 * OWNERS * GROUPS), 2) void prompt_fwd_kernel(c
 #pragma unroll
     for (int r = 0; r < 16; ++r) o[d][r] = 0.f;
   float m = -INFINITY, neg_m = 0.f, l = 0.f;
-  NotFinite not_finite;
+  NotFinite plain;
 
   if (group < ntile) fetch(group, 0);
   bf16x8 qf[KS];
@@ -139,7 +142,7 @@ __global__ __launch_bounds__((64 * OWNERS * GROUPS), 2) void prompt_fwd_kernel(c
     const uint32_t kt_ = tiles + buf * 2 * TILE_BYTES, vt_ = kt_ + TILE_BYTES;
     if (j0 + TILE_KEYS > full) {
 #pragma unroll
-      for (int u = 0; u < TILE_BYTES / (1024 * OWNERS); ++u) not_finite.look(lds_read<u32x4>(vt_ + u * 1024 * OWNERS + tid * 16));
+      for (int u = 0; u < TILE_BYTES / (1024 * OWNERS); ++u) plain.look(lds_read<u32x4>(vt_ + u * 1024 * OWNERS + tid * 16));
     }
     if (j0 >= wave_kend) continue;
     lds.fresh();
@@ -170,6 +173,7 @@ __global__ __launch_bounds__((64 * OWNERS * GROUPS), 2) void prompt_fwd_kernel(c
       m = mn;
       neg_m = -ms;
       l *= alpha;
+      plain.mark(fabsf(ms) >= kFar);
 #pragma unroll
       for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -198,8 +202,8 @@ __global__ __launch_bounds__((64 * OWNERS * GROUPS), 2) void prompt_fwd_kernel(c
   }
 
   float* lse = a.lse ? a.lse + (int64_t)head * a.Tq + sq.first : nullptr;
-  // rows of V that not all queries may see hold infinities or NaN: 0 times those is NaN
-  if (full < ntile * TILE_KEYS && __syncthreads_or(not_finite.found())) {
+  // rows of V that not all queries may see hold infinities or NaN: 0 times those is NaN; or a maximum is too far from 0
+  if (__syncthreads_or(plain.found())) {
     for (int r = group; r < min(32, nq - i0); r += GROUPS) {
       const int row = i0 + r;
       slow_row<DH>(a.Q.p + (int64_t)(sq.first + row) * a.Q.row + (int64_t)head * a.Q.head, kbase, a.K.row, vbase, a.V.row,

@@ -48,3 +48,28 @@ def test_decode_small_keys_and_large_scales(fmt, width, std, scale):
     k, v = (ref.f64(t) if fmt == attn.CACHE_BF16 else ref.values(*ref.quantise(ref.f64(t))) for t in (K, V))
     want = ref.prompt(ref.f64(Q), k, v, [1, 1], lens, False, scale)["Y"]
     ref.check("Y", attn.decode(shape, Q.cuda(), cache, table, ints(lens), scale=scale), *want)
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("log2", [10, 15, 20, 30, 60, 100])
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("H,Hk,lens", [(2, 1, [100, 90]), (64, 64, [100, 128]), (2, 2, [300, 256]), (16, 16, [300, 256])])
+def test_prompt_scores_far_from_0(H, Hk, lens, dh, log2, causal):
+    """Whole numbers times a power of two, so that scores are exact: of the largest, which are that far apart, Y is the mean,
+    and nothing of the others is left."""
+    T, g = sum(lens), torch.Generator().manual_seed(log2)
+    whole = lambda h: torch.randint(-8, 9, (T, h, dh), generator=g).to(torch.bfloat16)
+    Q, K, V = whole(H) * 2.0 ** (log2 // 2), whole(Hk) * 2.0 ** (log2 - log2 // 2), ref.bf16(T, Hk, dh, seed=5)
+    shape, cu = attn.make_shape(len(lens), T, T, H, Hk, dh, causal, 1.0), ref.sums(lens).cuda()
+    Y, lse = attn.prompt_fwd(shape, Q.cuda(), K.cuda(), V.cuda(), cu, cu)
+    q, k, v = map(ref.f64, (Q, K, V))
+    at = 0
+    for n in lens:
+        rows, seen = slice(at, at + n), ref.visible(n, n, causal)
+        for h in range(H):
+            p, want = ref.softmax(q[rows, h] @ k[rows, h // (H // Hk)].T, seen)
+            y = p @ v[rows, h // (H // Hk)]
+            # (p are 1 / n of n equal ones, which P's rounding does not tell apart: it and that of the sum are in 3 U)
+            ref.check(f"Y, head {h}", ref.f64(Y)[rows, h], y, 3 * ref.U * p @ np.abs(v[rows, h // (H // Hk)]))
+            ref.check(f"lse, head {h}", ref.f64(lse)[h, rows], want, np.abs(want) * 2.0 ** -21 + 2.0 ** -18)
+        at += n
