@@ -6,7 +6,8 @@
  *
  * Conventions are those of spt.h: device pointers unless they say "host"; every call validates on
  * the host, enqueues on `stream` (a hipStream_t), never synchronises, never allocates; outputs are
- * overwritten; same inputs give bit-identical outputs (no floating-point atomics).  Return codes are
+ * overwritten; same calls give bit-identical outputs (no floating-point atomics; the order of sums, and so a sequence's last
+ * bits, may change with the sizes of the call that it is in).  Return codes are
  * those of spt.h (SPT_OK, SPT_ERR_ARG, SPT_ERR_UNSUPPORTED, SPT_ERR_WORKSPACE, SPT_ERR_HIP).
  * Calls on several streams may overlap as long as they share no output and no workspace.  Outputs and workspaces share no
  * memory with one another or with inputs.  What is not finite among the keys and values that a query sees makes what depends on
@@ -32,7 +33,7 @@ extern "C" {
 typedef struct {
   int32_t B;      /* sequences, 1 .. 4096; any of them may be empty */
   int32_t Tq, Tk; /* rows of Q, of K and V: at least one; cu_q[B] <= Tq, cu_k[B] <= Tk */
-  int32_t H, Hk;  /* query heads (at most 65535; B H and Tq H / 128 together below 2^23), key heads */
+  int32_t H, Hk;  /* query heads, at most 65535, and key heads; Tq H / 128 + B H and (Tk / 128 + B) Hk at most 2^23 - 16 */
   int32_t dh;     /* 64 or 128 */
   int32_t causal; /* 0 or 1 */
   float scale;    /* logits are scale * q.k; positive, at most 2e38 */
@@ -41,7 +42,8 @@ typedef struct {
 /* y_i = sum_j p_ij v_j, p_ij = exp(s_ij - lse_i), s_ij = scale q_i.k_j, lse_i = log sum_j exp(s_ij),
  * over the keys that query i sees.  A query that sees none (or none with a score above -inf) gets
  * y = 0 and lse = -inf.  Keys that a query does not see do not touch its row, whatever they hold
- * (infinities and NaN included); rows of Y and lse behind cu_q[B] are left as they were.
+ * (infinities and NaN included); rows of Y and lse behind cu_q[B] are left as they were.  Scores may have any size that fp32
+ * holds; tiles with one above 2^28 are taken a row at a time.
  *   Q, Y    bf16 [Tq][H][dh]     K, V  bf16 [Tk][Hk][dh]     (16-byte aligned)
  *   strides host, or NULL for dense tensors: elements from a row to the next and from a head to the
  *           next, of Q, K, V, Y: 8 numbers.  Multiples of 8, not negative, below 2^23; dh is
@@ -59,8 +61,10 @@ int spt_attn_prompt_fwd(const spt_attn_shape_t* shape, const void* Q, const void
  * A query that sees no key has dq = 0, a key that no query sees dk = dv = 0; rows behind cu_q[B], cu_k[B] are left as they were.
  *   strides  host, or NULL: of Q, K, V, Y, dY, dQ, dK, dV: 16 numbers
  *   ws       spt_attn_prompt_workspace_bytes(shape) bytes, 256-byte aligned
- * In front of their products P is rounded to bf16, dS to bf16 or, where there are few rows, to the sum of two.  What the
- * rounding of Y leaves in the sum of a row's dS, which is 0, is taken off D. */
+ * In front of their products P is rounded to bf16, dS to bf16 or, where there are few rows (Tq H <= 128 B Hk or
+ * (Tq / 32) H <= 256, by the sizes of the call: a sequence alone may have the one, in a large batch the other), to the sum of two.  What the
+ * rounding of Y leaves in the sum of a row's dS, which is 0, is taken off D.  P comes from scores and an lse of 32 bits: it is off by up to
+ * |lse| 2^-22 of itself, bf16's rounding at 2^14; from 2^29 on gradients may not be finite. */
 int spt_attn_prompt_bwd(const spt_attn_shape_t* shape, const void* Q, const void* K, const void* V,
                         const void* Y, const void* dY, const float* lse, const int64_t* strides,
                         const int32_t* cu_q, const int32_t* cu_k, void* dQ, void* dK, void* dV, void* ws,
@@ -81,7 +85,7 @@ size_t spt_attn_prompt_workspace_bytes(const spt_attn_shape_t* shape);
 typedef struct {
   int32_t pages;     /* pages of the pool */
   int32_t page;      /* tokens of a page: 16, 32, 64, 128 or 256 */
-  int32_t Hk, dh;
+  int32_t Hk, dh;    /* Hk at most 65535 */
   int32_t format;    /* SPT_CACHE_BF16 or SPT_CACHE_E4M3 */
   int32_t B;         /* sequences, 1 .. 65535 */
   int32_t max_pages; /* row length of table: a sequence has at most max_pages * page tokens (below 2^31) */
@@ -113,7 +117,11 @@ int spt_cache_read(const spt_cache_shape_t* shape, int32_t T, void* K, void* V, 
  *   Q, Y bf16 [B][H][dh];  strides host, or NULL for dense: of Q, Y: 4 numbers, as above
  *   lens int32 [B];  scale positive, at most 2e38
  *   ws: spt_attn_decode_workspace_bytes(shape, H) bytes, 256-byte aligned
- * B * Hk * ceil(max_pages * page / 32) * ceil(H / Hk / 16) must be below 2^31, B * H below 2^23 - 16. */
+ * H is at most 65535, B * Hk * ceil(max_pages * page / 32) * ceil(H / Hk / 16) below 2^31, B * H at most 2^23 - 16.
+ * Sixteen query heads of a key head are taken at a time: where more share one, its part of the cache is read again for every sixteen.
+ * In tables of many tokens the lengths are gone through for every sequence and head: 4096 sequences of 64 tokens, 8 heads on 2,
+ * take 2.7 times as long as in a table of 64 tokens, 16384 take 8 times as long.  Of values below 2^-117 that are held in 8 bits
+ * the products with their weights lose bits. */
 int spt_attn_decode(const spt_cache_shape_t* shape, int32_t H, float scale, const void* Q, const int64_t* strides,
                     const void* Kc, const void* Vc, const uint8_t* ks, const uint8_t* vs, const int32_t* table,
                     const int32_t* lens, void* Y, void* ws, size_t ws_bytes, void* stream);

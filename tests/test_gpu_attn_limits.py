@@ -73,3 +73,20 @@ def test_prompt_scores_far_from_0(H, Hk, lens, dh, log2, causal):
             ref.check(f"Y, head {h}", ref.f64(Y)[rows, h], y, 3 * ref.U * p @ np.abs(v[rows, h // (H // Hk)]))
             ref.check(f"lse, head {h}", ref.f64(lse)[h, rows], want, np.abs(want) * 2.0 ** -21 + 2.0 ** -18)
         at += n
+
+
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("log2", [4, 9, 12, 14])
+def test_gradients_of_large_scores(dh, log2):
+    """Sequences of one token: P is 1, off by |lse| 2^-22 (three roundings of 2^-24 and those of ln 2 and its reciprocal) and its
+    rounding, and dV is rounded too."""
+    n, H, Hk = 200, 4, 2
+    Q, K, V, dY = (ref.bf16(n, h, dh, seed=seed) for seed, h in ((1, H), (2, Hk), (3, Hk), (4, H)))
+    shape, cu = attn.make_shape(n, n, n, H, Hk, dh, True, 2.0 ** log2 / dh), ints(list(range(n + 1)))
+    Q, K, V, dY = (t.cuda() for t in (Q, K, V, dY))
+    Y, lse = attn.prompt_fwd(shape, Q, K, V, cu, cu)
+    assert torch.equal(Y, V.repeat_interleave(2, 1))
+    dV = ref.f64(attn.prompt_bwd(shape, Q, K, V, Y, dY, lse, cu, cu)[2])
+    dy, far = ref.f64(dY), np.abs(ref.f64(lse)).T[:, :, None] * 2.0 ** -22
+    pairs = lambda x: x[:, 0::2] + x[:, 1::2]                        # the two heads of a key head
+    ref.check("dV", dV, pairs(dy), ref.U * np.abs(pairs(dy)) + 1.02 * pairs((ref.U + far) * np.abs(dy)))
