@@ -152,8 +152,9 @@ __global__ __launch_bounds__(256) void cache_read_kernel(const RowArgs a) {
 }
 
 // ------------------------------------------------------------------------------------------
-// Decoding.  The cache is read once; everything else is small.  An item is a key head of a sequence with up to 16 of the
-// query heads that read it (the columns of a 16 x 16 x 32 product), a unit 32 tokens of an item.  The units of all items stand in one
+// Decoding.  The cache is read once for every sixteen query heads of a key head; everything else is small.  An item is a key head of a sequence
+// with up to 16 of the query heads that read it (the columns of a 16 x 16 x 32 product), a unit 32 tokens of an item.  (More heads read it
+// again, as items of their own: 8 sequences of 8000, one key head of 128 in 16 bits, 16 heads 22.6 us, 32 25.5, 64 33.7, 128 52.3.)  The units of all items stand in one
 // line, and every wavefront takes an equal stretch of it, whatever the lengths: an item that lies within one stretch is
 // finished there, the others leave a partial result (maximum, sum, unnormalised output) per stretch, which a second launch
 // joins in the order of the cache.  At most the first and the last item of a stretch are partial: two slots a stretch.
@@ -329,7 +330,7 @@ struct DecodeState {
 };
 
 // Asynchronous copies of unit t of a sequence into a stage; returns which of its 32 tokens are there.  Nobody reads a row again in the launch
-// (two sets of a group's heads do): kept in L2 48 sequences of 100 to 8000 tokens in 8 bits, 32 heads of 128 on 8, went in 45.8 us, 41.2 so,
+// (but for groups of more than sixteen heads): kept in L2 48 sequences of 100 to 8000 tokens in 8 bits, 32 heads of 128 on 8, went in 45.8 us, 41.2 so,
 // six of 30000 to 32700 in 16 bits in 137 (5.6 TB/s) and 121 (6.4).
 template <int DH, bool E4M3>
 __device__ __forceinline__ uint32_t fetch_unit(const DecodeArgs& a, int hk, int t, int len, const int* page, uint32_t at, uint32_t exponents, int lane) {
@@ -587,7 +588,8 @@ __global__ __launch_bounds__((64 * ItemTile<DH, E4M3>::WAVES), 2) void decode_it
 }
 
 // A workgroup per query head: the partial results of its item in the order of the cache, or zeros without a key.  Eight (dh 128) or
-// sixteen parts of the list side by side, joined in order.
+// sixteen parts of the list side by side, joined in order.  Each finds its item's stretches from all lengths, work that grows with
+// the square of the sequences: 8 heads of 128 on 2, 64 tokens each, 64 sequences 6.4 us, 1024 25, 4096 244, 16384 3636 (their units 8.3, 20, 74, 296).
 template <int DH>
 __global__ __launch_bounds__(256) void decode_join_kernel(const DecodeArgs a) {
   constexpr int LANES = DH / 4, PARTS = 256 / LANES;
@@ -732,7 +734,7 @@ hipError_t launch_items(const DecodeArgs& a, hipStream_t st) {
 }
 
 // Whether a table is so narrow that a wavefront of an item's workgroup has four units at most: then the launch of the joins costs more than
-// an even split gains.  us a call in a graph, stretches and items, 32 heads on 8 of 128: 32 sequences of 512 tokens 17.3 and 12.4, one of
+// an even split gains, but for a few sequences that fill it (the width is what is known on the host).  us a call in a graph, stretches and items, 32 heads on 8 of 128: 32 sequences of 512 tokens 17.3 and 12.4, one of
 // them 8.8 and 8.5, 64 of 10 to 1000 in 8 bits 16.4 and 15.9, 16 of 1000 14.2 and 11.7, 4 of them 10.2 and 11.7; one sequence of 100, 32 heads
 // of 64: 8.3 and 4.2.  Wider tables: one of 1024 in 16 bits (four wavefronts) 9.4 and 13.6, one of 2048 in 8 bits 9.4 and 17.6.
 bool short_table(const spt_cache_shape_t& s) {

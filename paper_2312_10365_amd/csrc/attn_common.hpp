@@ -79,7 +79,8 @@ inline int64_t row_workgroups(int T, int shift, int B, int heads) { return (int6
 // and 64-wide heads, of which one workgroup of four leaves a CU's wavefronts waiting.  us, four owners and two, `causal`: 8 heads, 4000 tokens (500
 // workgroups), of 64 forward 44 and 34, query side 89 and 49, key side 105 and 55, of 128 58 and 54, 132 and 81, 114 and 87; 31 sequences of 4 to
 // 1993, 4 heads of 64 on 2 key side 109 and 49; 4 of 512, 16 heads of 64 query side 19.2 and 21.6; two of 4000, 8 heads of 128 (1000) key side
-// 137 and 169.  All keys seen: 8 heads of 64, 4000 48 and 50, 90 and 81, 105 and 91, of 128 69 and 88, 142 and 137, 129 and 150.
+// 137 and 169.  All keys seen: 8 heads of 64, 4000 48 and 50, 90 and 81, 105 and 91, of 128 69 and 88, 142 and 137, 129 and 150 (one rule for three kernels: the
+// forward's 2 us at 64 are less than the other two gain).
 inline int row_owners(int T, int heads, int hshift, int64_t through, const spt_attn_shape_t& s) {
   const int hs = hshift < 1 ? hshift : 1;
   const int64_t ones = row_workgroups(T, 5, s.B, heads), twos = row_workgroups(T, 6 - hs, s.B, heads >> hs), B = s.B;

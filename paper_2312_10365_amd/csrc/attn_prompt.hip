@@ -8,6 +8,8 @@
 // maximum, sum and rescaling of a query are one lane's (two halves of a row meet in one lane swap).  O^T = V^T P^T takes V out of LDS
 // through the transposing read.  One pass over the keys: running maximum m and sum l, p = 2^(c s - m) with c = scale log2 e; the
 // accumulators are rescaled only when a maximum rises by more than 2^8 (p stays below 256, and the sums are fp32).
+// P goes into its product as one bf16, the sum that divides is that of the exact p: Y is 1.9e-3 off (2-norm; 150 tokens, 8 heads of 64; the
+// rounding of Y alone makes 1.6e-3).  As the sum of two it was 1.6e-3, for a product more: 8192 tokens, 32 heads of 128 on 8, 528 us so, 710 with two.
 #include <algorithm>
 #include <type_traits>
 

@@ -13,6 +13,8 @@
 // Where there is little to do, four or eight groups of wavefronts share what passes through LDS for the same 32 or 64 rows, and their sums are
 // added in order.
 // S and dP are formed in both: the alternative, keeping dS or partial dQ in memory, moves as many bytes as it saves time.
+// P goes into dV's product as one bf16: dV is 2.3e-3 off (2-norm), as dK is with dS so, where its own rounding makes 1.66e-3.  As the sum of two
+// 1.66e-3, key side 71 and 77 us (16 sequences of 512, 32 heads of 64), 495 and 575 (six of 500 to 4000, 32 heads of 128 on 8).
 #include <algorithm>
 #include <type_traits>
 
