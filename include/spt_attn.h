@@ -42,8 +42,8 @@ typedef struct {
 /* y_i = sum_j p_ij v_j, p_ij = exp(s_ij - lse_i), s_ij = scale q_i.k_j, lse_i = log sum_j exp(s_ij),
  * over the keys that query i sees.  A query that sees none (or none with a score above -inf) gets
  * y = 0 and lse = -inf.  Keys that a query does not see do not touch its row, whatever they hold
- * (infinities and NaN included); rows of Y and lse behind cu_q[B] are left as they were.  Scores may have any size that fp32
- * holds; tiles with one above 2^28 are taken a row at a time.
+ * (infinities and NaN included); rows of Y and lse behind cu_q[B] are left as they were.  q.k and the scores may have any size that
+ * fp32 holds (scores: times log2 e); rows of a workgroup that meets one above 2^27 are taken one by one.
  *   Q, Y    bf16 [Tq][H][dh]     K, V  bf16 [Tk][Hk][dh]     (16-byte aligned)
  *   strides host, or NULL for dense tensors: elements from a row to the next and from a head to the
  *           next, of Q, K, V, Y: 8 numbers.  Multiples of 8, not negative, below 2^23; dh is
