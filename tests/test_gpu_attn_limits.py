@@ -90,3 +90,23 @@ def test_gradients_of_large_scores(dh, log2):
     dy, far = ref.f64(dY), np.abs(ref.f64(lse)).T[:, :, None] * 2.0 ** -22
     pairs = lambda x: x[:, 0::2] + x[:, 1::2]                        # the two heads of a key head
     ref.check("dV", dV, pairs(dy), ref.U * np.abs(pairs(dy)) + 1.02 * pairs((ref.U + far) * np.abs(dy)))
+
+
+@pytest.mark.parametrize("fmt", [attn.CACHE_BF16, attn.CACHE_E4M3])
+@pytest.mark.parametrize("width", [32, 300])
+@pytest.mark.parametrize("log2", [10, 30, 60, 100])
+def test_decode_scores_far_from_0(log2, width, fmt):
+    """As in prompts: of the largest scores Y is the mean, over one launch and over joined stretches."""
+    n, page, Hk, dh, g = 500, 16, 2, 64, torch.Generator().manual_seed(log2)
+    whole = lambda *shape: torch.randint(-8, 9, (*shape, dh), generator=g).to(torch.bfloat16)
+    Q, K, V = whole(1, 4) * 2.0 ** (log2 // 2), whole(n, Hk) * 2.0 ** (log2 - log2 // 2), ref.bf16(n, Hk, dh, seed=5)
+    table = torch.full((1, width), -1, dtype=torch.int32)
+    table[0, :32] = torch.arange(32)
+    shape, table = attn.make_cache_shape(32, page, Hk, dh, 1, width, fmt), table.cuda()
+    cache = attn.alloc_cache(shape)
+    attn.cache_write(shape, K.cuda(), V.cuda(), cache, table, ints([0]), ints([0, n]))
+    Y = ref.f64(attn.decode(shape, Q.cuda(), cache, table, ints([n]), scale=1.0))[0]
+    k, v = (ref.f64(t) if fmt == attn.CACHE_BF16 else ref.values(*ref.quantise(ref.f64(t))) for t in (K, V))
+    for h in range(4):
+        p, _ = ref.softmax(ref.f64(Q)[:, h] @ k[:, h // 2].T, np.ones((1, n), bool))
+        ref.check(f"Y, head {h}", Y[h], (p @ v[:, h // 2])[0], (2 * ref.U * p @ np.abs(v[:, h // 2]))[0])
